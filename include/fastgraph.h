@@ -252,6 +252,82 @@ fg_status fg_oc_helper(const int32_t* asso_idx, const int32_t* unique_idx, const
                        int32_t n_maxrs, int32_t calc_m_not, int32_t rot_block, int32_t* M, int32_t* M_not,
                        void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Rows by index ----------------------------------------------------------------------------------------------------
+ * What a network does with an index once it has one, a graph's neighbours, tokens, or choices of experts: fetch the rows
+ * that it names, weigh and sum them, and send gradients back.
+ *
+ * Rows are c elements of one type; `*_stride` is the number of elements from a row to the next (outputs: >= c, inputs: any, 0
+ * too; what lies between two rows is neither read nor written).  Pointers need the alignment of an element.  Weights are float32.  An index entry outside
+ * 0..n_rows-1 (a neighbour list's padding, -1) names no row.  Sums are float32, in the order of the index's entries, and
+ * rounded once to the type of the output: the same bits in every run.  Outputs must not overlap inputs.
+ *   1 <= c <= FG_MAX_C, strides <= FG_MAX_STRIDE, 1 <= k <= FG_MAX_K; rows, index entries (t * k) <= FG_MAX_N
+ * Errors besides those of the other calls: FG_ERR_UNSUPPORTED for an unknown type or a pointer that an element of its type
+ * may not have.  The sorted form of an index (order, bounds) must be fg_index_sort's of that index with that n_rows. */
+typedef enum {
+    FG_F32 = 0,
+    FG_BF16 = 1,
+    FG_F16 = 2,
+    FG_TYPE_INT_RANGE = 0x7fffffff
+} fg_type;
+#define FG_MAX_C (1 << 24)
+#define FG_MAX_STRIDE (1 << 29)
+
+/* Stable counting sort of an index by the row that it names (what fg_bin_points does for points and bins).
+ *   index  [m]
+ *   order  [m] out           entries in the order of their rows, those of one row ascending; entries that name no row last
+ *   place  [m] out, or NULL  where an entry is in that order; -1 for one that names no row
+ *   bounds [n_rows + 1] out  row v has the positions [bounds[v], bounds[v+1]); bounds[n_rows] entries name a row
+ * m == 0: bounds is zero.  workspace: fg_index_sort_workspace_size() bytes, 256-byte aligned; may be NULL where that is 0. */
+fg_status fg_index_sort_workspace_size(int64_t m, int64_t n_rows, size_t* bytes /* host out */);
+fg_status fg_index_sort(const int32_t* index, int64_t m, int64_t n_rows, int32_t* order, int32_t* place, int32_t* bounds,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* out[i] = scale * table[index[i]], a row of zeros where index[i] names none.
+ *   table [n_rows][c], index [m], out [m][c], all rows of `type`. */
+fg_status fg_lookup(const void* table, int32_t type, int64_t n_rows, int64_t c, int64_t table_stride, const int32_t* index,
+                    int64_t m, float scale, void* out, int64_t out_stride, void* stream);
+
+/* The table's gradient: grad_table[v] = scale * sum over the entries i of row v of grad_out[i], by the sorted index.
+ *   grad_out   [m][c] of `type`
+ *   grad_table [n_rows][c] of grad_type, `type` or FG_F32; all rows are written (zeros where no entry names one), or, with
+ *              accumulate != 0, the sums are added to what is there (float32, rounded once) and rows that no entry names are
+ *              not touched
+ * workspace: fg_lookup_backward_workspace_size() bytes, 256-byte aligned; may be NULL where that is 0. */
+fg_status fg_lookup_backward_workspace_size(int64_t m, int64_t c, int32_t type, size_t* bytes /* host out */);
+fg_status fg_lookup_backward(const void* grad_out, int32_t type, int64_t m, int64_t c, int64_t grad_stride, const int32_t* index,
+                             const int32_t* order, const int32_t* bounds, int64_t n_rows, float scale, int32_t accumulate,
+                             void* grad_table, int32_t grad_type, int64_t table_stride, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
+/* Rows into the order of an index with k entries a row: out[place[i][j]] = x[i], bit for bit.
+ *   x [t][c], place [t][k] (fg_index_sort's of the choices [t][k]: expert e's rows are then out[bounds[e] .. bounds[e+1])),
+ *   out [n_rows][c].  Rows of out that no entry names are left as they were; a row named twice gets one of the two.
+ * The gradient of x is fg_combine of the gradient of out by `place`, without weights. */
+fg_status fg_dispatch(const void* x, int32_t type, int64_t t, int64_t c, int64_t x_stride, const int32_t* place, int32_t k,
+                      int64_t n_rows, void* out, int64_t out_stride, void* stream);
+
+/* out[i] = sum over j of weights[i][j] * rows[index[i][j]]: experts' answers back to their tokens (index = place), or the
+ * message that a point receives from its neighbours (index = fg_binned_select_knn's out_idx).
+ *   rows [n_rows][c], index [t][k], weights [t][k] or NULL (all 1), out [t][c] of the rows' type.
+ * Entries that name no row add nothing, whatever their weight. */
+fg_status fg_combine(const void* rows, int32_t type, int64_t n_rows, int64_t c, int64_t rows_stride, const int32_t* index,
+                     const float* weights, int64_t t, int32_t k, void* out, int64_t out_stride, void* stream);
+
+/* Gradients of fg_combine:
+ *   grad_rows[v]       = sum over the entries (i, j) that name v of weights[i][j] * grad_out[i]
+ *   grad_weights[i][j] = <grad_out[i], rows[index[i][j]]>, 0 where the entry names no row
+ *   grad_out [t][c], rows [n_rows][c] (read for grad_weights only), grad_rows [n_rows][c] or NULL, grad_weights [t][k] or NULL;
+ *   rows of grad_out, rows and grad_rows are of `type`.
+ * order, bounds: both NULL: no row is named twice (index = place); rows that no entry names are left as they were, and a row that
+ * is named twice gets one of its terms.  Both given (fg_index_sort of index [t*k]): rows may be named any number of times, and
+ * all of grad_rows is written.
+ * workspace (with order and grad_rows only): fg_combine_backward_workspace_size() bytes, 256-byte aligned; NULL where that is 0. */
+fg_status fg_combine_backward_workspace_size(int64_t t, int32_t k, int64_t c, int32_t type, size_t* bytes /* host out */);
+fg_status fg_combine_backward(const void* grad_out, int32_t type, int64_t t, int64_t c, int64_t grad_stride, const void* rows,
+                              int64_t n_rows, int64_t rows_stride, const int32_t* index, const float* weights, int32_t k,
+                              const int32_t* order, const int32_t* bounds, void* grad_rows, int64_t grad_rows_stride,
+                              float* grad_weights, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -24,7 +24,9 @@ FG_ERR_LAUNCH = 5
 
 EXPORTS = ["fg_status_string", "fg_auto_n_bins", "fg_workspace_size", "fg_bin_points",
            "fg_binned_select_knn", "fg_binned_select_knn_static", "fg_binned_select_knn_dir", "fg_binned_select_knn_counted", "fg_query_binned",
-           "fg_knn_backward", "fg_knn_backward_binned", "fg_oc_helper", "fg_oc_helper_workspace_size"]
+           "fg_knn_backward", "fg_knn_backward_binned", "fg_oc_helper", "fg_oc_helper_workspace_size",
+           "fg_index_sort_workspace_size", "fg_index_sort", "fg_lookup", "fg_lookup_backward_workspace_size", "fg_lookup_backward",
+           "fg_dispatch", "fg_combine", "fg_combine_backward_workspace_size", "fg_combine_backward"]
 
 
 class FgError(RuntimeError):
@@ -86,6 +88,19 @@ def lib() -> ctypes.CDLL:
         L.fg_oc_helper.argtypes = [vp, vp, vp, vp, i64, i64, i32, i32, i32, i32, i32, vp, vp, vp, sz, vp]
         L.fg_oc_helper_workspace_size.restype = ctypes.c_int
         L.fg_oc_helper_workspace_size.argtypes = [i64, i32, ctypes.POINTER(sz)]
+        f32, psz = ctypes.c_float, ctypes.POINTER(sz)
+        for name, args in {
+                "fg_index_sort_workspace_size": [i64, i64, psz],
+                "fg_index_sort": [vp, i64, i64, vp, vp, vp, vp, sz, vp],
+                "fg_lookup": [vp, i32, i64, i64, i64, vp, i64, f32, vp, i64, vp],
+                "fg_lookup_backward_workspace_size": [i64, i64, i32, psz],
+                "fg_lookup_backward": [vp, i32, i64, i64, i64, vp, vp, vp, i64, f32, i32, vp, i32, i64, vp, sz, vp],
+                "fg_dispatch": [vp, i32, i64, i64, i64, vp, i32, i64, vp, i64, vp],
+                "fg_combine": [vp, i32, i64, i64, i64, vp, vp, i64, i32, vp, i64, vp],
+                "fg_combine_backward_workspace_size": [i64, i32, i64, i32, psz],
+                "fg_combine_backward": [vp, i32, i64, i64, i64, vp, i64, i64, vp, vp, i32, vp, vp, vp, i64, vp, vp, sz, vp]}.items():
+            fn = getattr(L, name)
+            fn.restype, fn.argtypes = ctypes.c_int, args
         _lib = L
     return _lib
 
@@ -390,3 +405,207 @@ def fg_oc_helper(asso_idx: torch.Tensor, unique_idx: torch.Tensor, unique_rs_ass
                               _ptr(M), _ptr(M_not) if calc_m_not else 0, _ptr(workspace),
                               0 if workspace is None else workspace.numel(), _stream()), "fg_oc_helper")
     return M, (M_not if calc_m_not else None)
+
+
+# ---- rows by index ----
+
+FG_F32, FG_BF16, FG_F16 = 0, 1, 2
+_TYPES = {torch.float32: FG_F32, torch.bfloat16: FG_BF16, torch.float16: FG_F16}
+
+
+def _row_view(t: torch.Tensor, name: str, dtype=None, device=None, shape=None):
+    """(pointer, elements from a row to the next) of a 2-d tensor whose rows are contiguous."""
+    if not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    if t.dim() != 2 or (dtype is not None and t.dtype != dtype) or t.dtype not in _TYPES:
+        raise ValueError("%s must be 2-d %s" % (name, dtype or "float32, bfloat16 or float16"))
+    n, c = t.shape
+    if shape is not None and (n, c) != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), (n, c)))
+    if device is not None and t.device != device:
+        raise ValueError("%s must be on %s" % (name, device))
+    stride, one = t.stride()
+    if one != 1 and c > 1 and n > 0:
+        raise ValueError("%s must have contiguous rows" % name)
+    return _ptr(t), (stride if n > 1 else c)
+
+
+def _index(t: torch.Tensor, name: str, device, dims=None) -> int:
+    _dev(t, torch.int32, name)
+    if t.device != device:
+        raise ValueError("%s must be on %s" % (name, device))
+    if dims is not None and t.dim() != dims:
+        raise ValueError("%s must be %d-d" % (name, dims))
+    return _ptr(t)
+
+
+def _weights(t, shape, device, name: str) -> int:
+    if t is None:
+        return 0
+    _dev(t, torch.float32, name)
+    if t.shape != shape or t.device != device:
+        raise ValueError("%s must have shape %s and be on %s" % (name, tuple(shape), device))
+    return _ptr(t)
+
+
+def _call(name: str, device, *args):
+    """The library's call on the device's current stream, with that device current."""
+    stream = torch.cuda.current_stream(device).cuda_stream
+    if device.index == torch.cuda.current_device():
+        _check(getattr(lib(), name)(*args, stream), name)
+    else:
+        with torch.cuda.device(device):
+            _check(getattr(lib(), name)(*args, stream), name)
+
+
+def _scratch(workspace, size: int, device):
+    if workspace is None:
+        return torch.empty(size, dtype=torch.uint8, device=device) if size else None
+    if not workspace.is_cuda or workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous and on %s" % (device,))
+    return workspace
+
+
+def _bytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def _sizes(name: str, *args) -> int:
+    out = ctypes.c_size_t(0)
+    _check(getattr(lib(), name)(*args, ctypes.byref(out)), name)
+    return int(out.value)
+
+
+def fg_index_sort_workspace_size(m: int, n_rows: int) -> int:
+    return _sizes("fg_index_sort_workspace_size", m, n_rows)
+
+
+def fg_lookup_backward_workspace_size(m: int, c: int, dtype: torch.dtype) -> int:
+    return _sizes("fg_lookup_backward_workspace_size", m, c, _TYPES[dtype])
+
+
+def fg_combine_backward_workspace_size(t: int, k: int, c: int, dtype: torch.dtype) -> int:
+    return _sizes("fg_combine_backward_workspace_size", t, k, c, _TYPES[dtype])
+
+
+@dataclass
+class IndexSort:
+    """An index in the order of the rows that it names (fg_index_sort)."""
+    index: torch.Tensor         # as it was given
+    n_rows: int
+    order: torch.Tensor         # [m] entries by row, ascending inside a row; those that name no row last
+    bounds: torch.Tensor        # [n_rows + 1] positions of the rows
+    place: torch.Tensor | None  # shape of the index: position of every entry, -1 where it names no row
+
+
+def fg_index_sort(index: torch.Tensor, n_rows: int, place: bool = True, workspace: torch.Tensor | None = None) -> IndexSort:
+    """index: int32 of any shape; place=False: without the inverse order."""
+    dev = index.device
+    ptr = _index(index, "index", dev)
+    m = index.numel()
+    ws = _scratch(workspace, fg_index_sort_workspace_size(m, n_rows), dev)
+    order = torch.empty(m, dtype=torch.int32, device=dev)
+    bounds = torch.empty(n_rows + 1, dtype=torch.int32, device=dev)
+    at = torch.empty(index.shape, dtype=torch.int32, device=dev) if place else None
+    _call("fg_index_sort", dev, ptr, m, n_rows, _ptr(order), _ptr(at), _ptr(bounds), _ptr(ws), _bytes(ws))
+    return IndexSort(index, n_rows, order, bounds, at)
+
+
+def fg_lookup(table: torch.Tensor, index: torch.Tensor, scale: float = 1.0, out: torch.Tensor | None = None) -> torch.Tensor:
+    """scale * table[index] ([*index.shape, c]; out, if given, [index.numel(), c]); zeros where an entry names no row."""
+    dev = table.device
+    rows, stride = _row_view(table, "table")
+    names = _index(index, "index", dev)
+    m, c = index.numel(), table.shape[1]
+    given = out
+    if out is None:
+        out = torch.empty((m, c), dtype=table.dtype, device=dev)
+    to, to_stride = _row_view(out, "out", table.dtype, dev, (m, c))
+    _call("fg_lookup", dev, rows, _TYPES[table.dtype], table.shape[0], c, stride, names, m, scale, to, to_stride)
+    return out if given is not None or index.dim() == 1 else out.view(*index.shape, c)
+
+
+def fg_lookup_backward(grad_out: torch.Tensor, sort: IndexSort, scale: float = 1.0, grad_table: torch.Tensor | None = None,
+                       dtype: torch.dtype | None = None, accumulate: bool = False, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """The table's gradient [sort.n_rows, c] from grad_out [m, c] (or [*index.shape, c]) and the sorted index.  dtype of a gradient that is
+    allocated: grad_out's or float32.  accumulate: added to grad_table, which must then be given."""
+    dev = grad_out.device
+    c = grad_out.shape[-1]
+    m = sort.index.numel()
+    if grad_out.dim() != 2:
+        if grad_out.shape[:-1] != sort.index.shape:
+            raise ValueError("grad_out must be [*index.shape, c]")
+        grad_out = grad_out.view(m, c)
+    grad, stride = _row_view(grad_out, "grad_out", shape=(m, c))
+    index = _index(sort.index, "sort.index", dev)
+    if grad_table is None:
+        if accumulate:
+            raise ValueError("accumulate needs grad_table")
+        grad_table = torch.empty((sort.n_rows, c), dtype=dtype or grad_out.dtype, device=dev)
+    to, to_stride = _row_view(grad_table, "grad_table", dtype, dev, (sort.n_rows, c))
+    ws = _scratch(workspace, fg_lookup_backward_workspace_size(m, c, grad_out.dtype), dev)
+    _call("fg_lookup_backward", dev, grad, _TYPES[grad_out.dtype], m, c, stride, index, _ptr(sort.order), _ptr(sort.bounds), sort.n_rows, scale,
+          1 if accumulate else 0, to, _TYPES[grad_table.dtype], to_stride, _ptr(ws), _bytes(ws))
+    return grad_table
+
+
+def fg_dispatch(x: torch.Tensor, place: torch.Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
+    """out[place[i, j]] = x[i]; place [t, k] of fg_index_sort.  out: [n, c]; if it is not given, [t * k, c], in which rows that no entry
+    names are uninitialised."""
+    dev = x.device
+    rows, stride = _row_view(x, "x")
+    at = _index(place, "place", dev, 2)
+    t, k = place.shape
+    if x.shape[0] != t:
+        raise ValueError("place must be [%d, k]" % x.shape[0])
+    c = x.shape[1]
+    if out is None:
+        out = torch.empty((t * k, c), dtype=x.dtype, device=dev)
+    to, to_stride = _row_view(out, "out", x.dtype, dev, (out.shape[0], c))
+    _call("fg_dispatch", dev, rows, _TYPES[x.dtype], t, c, stride, at, k, out.shape[0], to, to_stride)
+    return out
+
+
+def fg_combine(rows: torch.Tensor, index: torch.Tensor, weights: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """out[i] = sum_j weights[i, j] * rows[index[i, j]]: [t, c] of the rows' dtype."""
+    dev = rows.device
+    at, stride = _row_view(rows, "rows")
+    names = _index(index, "index", dev, 2)
+    w = _weights(weights, index.shape, dev, "weights")
+    t, k = index.shape
+    n, c = rows.shape
+    if out is None:
+        out = torch.empty((t, c), dtype=rows.dtype, device=dev)
+    to, to_stride = _row_view(out, "out", rows.dtype, dev, (t, c))
+    _call("fg_combine", dev, at, _TYPES[rows.dtype], n, c, stride, names, w, t, k, to, to_stride)
+    return out
+
+
+def fg_combine_backward(grad_out: torch.Tensor, rows: torch.Tensor, index: torch.Tensor, weights: torch.Tensor | None = None,
+                        sort: IndexSort | None = None, grad_rows: torch.Tensor | None = None, grad_weights: torch.Tensor | None = None,
+                        workspace: torch.Tensor | None = None):
+    """(gradient of rows, gradient of weights or None where there are none).  sort: fg_index_sort(index, len(rows)), needed where entries
+    share rows; without it every row is named once at most, and rows that none names keep what grad_rows has (zeros if it is not given)."""
+    dev = rows.device
+    n, c = rows.shape
+    at, stride = _row_view(rows, "rows")
+    names = _index(index, "index", dev, 2)
+    t, k = index.shape
+    grad, grad_stride = _row_view(grad_out, "grad_out", rows.dtype, dev, (t, c))
+    w = _weights(weights, index.shape, dev, "weights")
+    order = bounds = size = 0
+    if sort is not None:
+        if sort.n_rows != n or sort.index.shape != index.shape or sort.index.device != dev:
+            raise ValueError("sort must be fg_index_sort's of index for %d rows" % n)
+        order, bounds = _ptr(sort.order), _ptr(sort.bounds)
+        size = fg_combine_backward_workspace_size(t, k, c, rows.dtype)
+    if grad_rows is None:
+        grad_rows = (torch.zeros if sort is None else torch.empty)((n, c), dtype=rows.dtype, device=dev)
+    to, to_stride = _row_view(grad_rows, "grad_rows", rows.dtype, dev, (n, c))
+    if grad_weights is None and weights is not None:
+        grad_weights = torch.empty((t, k), dtype=torch.float32, device=dev)
+    gw = _weights(grad_weights, index.shape, dev, "grad_weights")
+    ws = _scratch(workspace, size, dev)
+    _call("fg_combine_backward", dev, grad, _TYPES[rows.dtype], t, c, grad_stride, at, n, stride, names, w, k, order, bounds, to, to_stride, gw,
+          _ptr(ws), _bytes(ws))
+    return grad_rows, grad_weights

@@ -1,8 +1,10 @@
 // C-ABI entry points: argument validation, workspace layout, stage launches.
 #include <math.h>
+#include <initializer_list>
 #include <mutex>
 #include "fg_internal.hpp"
 #include "fg_order.hpp"
+#include "fg_rows.hpp"
 
 // Workspace of fg_binned_select_knn_static: device memory that belongs to the library, one copy per GPU, held
 // until the process ends.  In host code this name is only a handle for hipGetSymbolAddress, never an address.
@@ -510,6 +512,162 @@ fg_status fg_oc_helper(const int32_t* asso_idx, const int32_t* unique_idx, const
                                     n_maxuq, n_maxrs, calc_m_not ? 1 : 0, rot_block, M, M_not, (int32_t*)workspace,
                                     (hipStream_t)stream);
     return e == hipSuccess ? FG_OK : FG_ERR_LAUNCH;
+}
+
+// ---- rows by index ----
+
+static int64_t type_bytes(int32_t type) { return type == FG_F32 ? 4 : (type == FG_BF16 || type == FG_F16 ? 2 : 0); }
+static bool bad_count(int64_t n) { return n < 0 || n > FG_MAX_N; }
+
+// What every call on rows has to hold: a type, a width, output rows that do not overlap, byte offsets that fit 64 bits.
+static fg_status check_rows(int32_t type, int64_t c, std::initializer_list<int64_t> in_strides = {}, std::initializer_list<int64_t> out_strides = {})
+{
+    if (type_bytes(type) == 0) return FG_ERR_UNSUPPORTED;
+    if (c < 1 || c > FG_MAX_C) return FG_ERR_BAD_SHAPE;
+    for (const int64_t s : in_strides)
+        if (s < 0 || s > FG_MAX_STRIDE) return FG_ERR_BAD_SHAPE;
+    for (const int64_t s : out_strides)
+        if (s < c || s > FG_MAX_STRIDE) return FG_ERR_BAD_SHAPE;
+    return FG_OK;
+}
+static bool misaligned(int32_t type, std::initializer_list<const void*> rows)
+{
+    for (const void* p : rows)
+        if ((uintptr_t)p % (uintptr_t)type_bytes(type) != 0) return true;
+    return false;
+}
+static bool bad_workspace(const void* workspace, size_t have, size_t need)
+{
+    return need != 0 && (!workspace || (uintptr_t)workspace % kAlign != 0 || have < need);
+}
+static bool bad_fan(int64_t t, int32_t k) { return t < 0 || k < 1 || k > FG_MAX_K || t > FG_MAX_N / k; }
+static fg_status told(hipError_t e) { return e == hipSuccess ? FG_OK : FG_ERR_LAUNCH; }
+
+fg_status fg_index_sort_workspace_size(int64_t m, int64_t n_rows, size_t* bytes)
+{
+    if (!bytes) return FG_ERR_NULL;
+    if (bad_count(m) || bad_count(n_rows)) return FG_ERR_BAD_SHAPE;
+    *bytes = align_up(index_sort_workspace_bytes(m, n_rows));
+    return FG_OK;
+}
+
+fg_status fg_index_sort(const int32_t* index, int64_t m, int64_t n_rows, int32_t* order, int32_t* place, int32_t* bounds,
+                        void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (bad_count(m) || bad_count(n_rows)) return FG_ERR_BAD_SHAPE;
+    if (!bounds || (m > 0 && (!index || !order))) return FG_ERR_NULL;
+    if (bad_workspace(workspace, workspace_bytes, index_sort_workspace_bytes(m, n_rows))) return FG_ERR_WORKSPACE;
+    return told(launch_index_sort(index, m, n_rows, order, place, bounds, workspace, (hipStream_t)stream));
+}
+
+fg_status fg_lookup(const void* table, int32_t type, int64_t n_rows, int64_t c, int64_t table_stride, const int32_t* index,
+                    int64_t m, float scale, void* out, int64_t out_stride, void* stream)
+{
+    const fg_status st = check_rows(type, c, {table_stride}, {out_stride});
+    if (st != FG_OK) return st;
+    if (bad_count(m) || bad_count(n_rows)) return FG_ERR_BAD_SHAPE;
+    if (m == 0) return FG_OK;
+    if (!index || !out || (!table && n_rows > 0)) return FG_ERR_NULL;
+    if (misaligned(type, {table, out})) return FG_ERR_UNSUPPORTED;
+    return told(launch_lookup(type, {table, table_stride}, n_rows, c, index, m, scale, {out, out_stride}, (hipStream_t)stream));
+}
+
+fg_status fg_lookup_backward_workspace_size(int64_t m, int64_t c, int32_t type, size_t* bytes)
+{
+    if (!bytes) return FG_ERR_NULL;
+    const fg_status st = check_rows(type, c);
+    if (st != FG_OK) return st;
+    if (bad_count(m)) return FG_ERR_BAD_SHAPE;
+    *bytes = align_up(row_sums_workspace_bytes(type, m, c));
+    return FG_OK;
+}
+
+fg_status fg_lookup_backward(const void* grad_out, int32_t type, int64_t m, int64_t c, int64_t grad_stride, const int32_t* index,
+                             const int32_t* order, const int32_t* bounds, int64_t n_rows, float scale, int32_t accumulate,
+                             void* grad_table, int32_t grad_type, int64_t table_stride, void* workspace, size_t workspace_bytes,
+                             void* stream)
+{
+    const fg_status st = check_rows(type, c, {grad_stride}, {table_stride});
+    if (st != FG_OK) return st;
+    if (grad_type != type && grad_type != FG_F32) return FG_ERR_UNSUPPORTED;
+    if (bad_count(m) || bad_count(n_rows)) return FG_ERR_BAD_SHAPE;
+    if (n_rows == 0) return FG_OK;
+    if (!bounds || !grad_table || (m > 0 && (!grad_out || !index || !order))) return FG_ERR_NULL;
+    if (misaligned(type, {grad_out}) || misaligned(grad_type, {grad_table})) return FG_ERR_UNSUPPORTED;
+    if (bad_workspace(workspace, workspace_bytes, row_sums_workspace_bytes(type, m, c))) return FG_ERR_WORKSPACE;
+    RowSums a = {};
+    a.type = type; a.out_type = grad_type;
+    a.grad = {grad_out, grad_stride}; a.out = {grad_table, table_stride};
+    a.index = index; a.order = order; a.bounds = bounds;
+    a.m = m; a.n_rows = n_rows; a.c = c; a.fan = 1; a.scale = scale; a.accumulate = accumulate;
+    a.partials = (float*)workspace;
+    return told(launch_row_sums(a, (hipStream_t)stream));
+}
+
+fg_status fg_dispatch(const void* x, int32_t type, int64_t t, int64_t c, int64_t x_stride, const int32_t* place, int32_t k,
+                      int64_t n_rows, void* out, int64_t out_stride, void* stream)
+{
+    const fg_status st = check_rows(type, c, {x_stride}, {out_stride});
+    if (st != FG_OK) return st;
+    if (bad_fan(t, k) || bad_count(n_rows)) return FG_ERR_BAD_SHAPE;
+    if (t == 0 || n_rows == 0) return FG_OK;
+    if (!x || !place || !out) return FG_ERR_NULL;
+    if (misaligned(type, {x, out})) return FG_ERR_UNSUPPORTED;
+    return told(launch_dispatch(type, {x, x_stride}, t, c, place, k, n_rows, {out, out_stride}, (hipStream_t)stream));
+}
+
+fg_status fg_combine(const void* rows, int32_t type, int64_t n_rows, int64_t c, int64_t rows_stride, const int32_t* index,
+                     const float* weights, int64_t t, int32_t k, void* out, int64_t out_stride, void* stream)
+{
+    const fg_status st = check_rows(type, c, {rows_stride}, {out_stride});
+    if (st != FG_OK) return st;
+    if (bad_fan(t, k) || bad_count(n_rows)) return FG_ERR_BAD_SHAPE;
+    if (t == 0) return FG_OK;
+    if (!index || !out || (!rows && n_rows > 0)) return FG_ERR_NULL;
+    if (misaligned(type, {rows, out})) return FG_ERR_UNSUPPORTED;
+    return told(launch_combine(type, {rows, rows_stride}, n_rows, c, index, weights, t, k, {out, out_stride}, (hipStream_t)stream));
+}
+
+fg_status fg_combine_backward_workspace_size(int64_t t, int32_t k, int64_t c, int32_t type, size_t* bytes)
+{
+    if (!bytes) return FG_ERR_NULL;
+    const fg_status st = check_rows(type, c);
+    if (st != FG_OK) return st;
+    if (bad_fan(t, k)) return FG_ERR_BAD_SHAPE;
+    *bytes = align_up(row_sums_workspace_bytes(type, t * k, c));
+    return FG_OK;
+}
+
+fg_status fg_combine_backward(const void* grad_out, int32_t type, int64_t t, int64_t c, int64_t grad_stride, const void* rows,
+                              int64_t n_rows, int64_t rows_stride, const int32_t* index, const float* weights, int32_t k,
+                              const int32_t* order, const int32_t* bounds, void* grad_rows, int64_t grad_rows_stride,
+                              float* grad_weights, void* workspace, size_t workspace_bytes, void* stream)
+{
+    fg_status st = check_rows(type, c, {grad_stride});
+    if (st == FG_OK && grad_weights) st = check_rows(type, c, {rows_stride});
+    if (st == FG_OK && grad_rows) st = check_rows(type, c, {}, {grad_rows_stride});
+    if (st != FG_OK) return st;
+    if (bad_fan(t, k) || bad_count(n_rows)) return FG_ERR_BAD_SHAPE;
+    if (!grad_rows && !grad_weights) return FG_OK;
+    const bool shared = order || bounds;
+    if (t > 0 && (!grad_out || !index || (grad_weights && !rows && n_rows > 0))) return FG_ERR_NULL;
+    if (shared && (!bounds || (t > 0 && !order))) return FG_ERR_NULL;
+    if (misaligned(type, {grad_out, rows, grad_rows})) return FG_ERR_UNSUPPORTED;
+    const bool sums = shared && grad_rows && n_rows > 0;
+    if (sums && bad_workspace(workspace, workspace_bytes, row_sums_workspace_bytes(type, t * k, c))) return FG_ERR_WORKSPACE;
+    if (sums) {
+        RowSums a = {};
+        a.type = type; a.out_type = type;
+        a.grad = {grad_out, grad_stride}; a.out = {grad_rows, grad_rows_stride};
+        a.index = index; a.order = order; a.bounds = bounds; a.weights = weights;
+        a.m = t * k; a.n_rows = n_rows; a.c = c; a.fan = k; a.scale = 1.0f;
+        a.partials = (float*)workspace;
+        if (launch_row_sums(a, (hipStream_t)stream) != hipSuccess) return FG_ERR_LAUNCH;
+    }
+    void* once = shared ? nullptr : grad_rows;
+    if (t == 0 || (!once && !grad_weights)) return FG_OK;
+    return told(launch_combine_grad(type, {grad_out, grad_stride}, t, c, {rows, rows_stride}, n_rows, index, weights, k,
+                                    {once, grad_rows_stride}, grad_weights, (hipStream_t)stream));
 }
 
 }  // extern "C"

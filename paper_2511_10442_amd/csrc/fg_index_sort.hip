@@ -1,0 +1,362 @@
+// Stable order of the entries of an index by the row that they name: order, place (its inverse) and bounds of the rows.
+//
+// A sort by digits from the lowest: every pass keeps the order that the one before made, so entries of one row stay as they came, and
+// sums over them come out the same in every run.  An entry outside 0..n_rows-1 has the key n_rows, behind all rows.  A pass of a tile:
+// 64 entries at a time a wavefront finds, with one ballot for every bit of the digit, which lanes have the same digit; the number of
+// those before a lane is its rank, their count moves the wavefront's counter of that digit.
+#include "fg_rows.hpp"
+
+namespace fg {
+
+namespace {
+
+constexpr int kMaxBits = 10;                 // of a digit: counters of a wavefront stay below 4 KiB of LDS
+constexpr int kSmallBlock = 1024;
+constexpr int64_t kSmallM = 8192;            // entries that one workgroup sorts in LDS
+constexpr int64_t kSmallRows = 4096;         // rows whose bounds that workgroup writes too
+constexpr int kBlock = 256;
+constexpr int kWaves = kBlock / 64;
+
+struct Plan { int bits, passes, items; int64_t tiles; };
+
+inline Plan plan_for(int64_t m, int64_t n_rows)
+{
+    Plan p;
+    int bits = 1;
+    while (((int64_t)1 << bits) <= n_rows) ++bits;       // keys 0..n_rows
+    p.passes = (bits + kMaxBits - 1) / kMaxBits;
+    p.bits = (bits + p.passes - 1) / p.passes;
+    p.items = m <= (1 << 20) ? 4 : 16;
+    p.tiles = (m + (int64_t)kBlock * p.items - 1) / ((int64_t)kBlock * p.items);
+    return p;
+}
+
+inline size_t up(size_t x) { return (x + 255) / 256 * 256; }
+
+struct Layout { size_t counts, totals, key_a, order_a, key_b, order_b, total; };
+
+inline Layout layout_for(int64_t m, const Plan& p)
+{
+    Layout l;
+    const size_t words = up((size_t)m * 4);
+    l.counts = 0;
+    l.totals = up(((size_t)1 << p.bits) * (size_t)p.tiles * 4);
+    l.key_a = l.totals + up(((size_t)1 << p.bits) * 4);
+    l.order_a = l.key_a + (p.passes > 1 ? words : 0);
+    l.key_b = l.order_a + (p.passes > 1 ? words : 0);
+    l.order_b = l.key_b + (p.passes > 1 ? words : 0);
+    l.total = l.order_b + (p.passes > 2 ? words : 0);
+    return l;
+}
+
+inline bool takes_small_sort(int64_t m) { return m <= kSmallM; }
+
+__device__ __forceinline__ uint32_t key_of(int32_t name, uint32_t n_rows) { return (uint32_t)name < n_rows ? (uint32_t)name : n_rows; }
+
+// Lanes of the wavefront whose digit is this lane's.
+__device__ __forceinline__ uint64_t same_digit(uint32_t digit, int bits, bool there)
+{
+    uint64_t peers = __ballot(there);
+    for (int b = 0; b < bits; ++b) {
+        const bool one = (digit >> b) & 1u;
+        const uint64_t ones = __ballot(one);
+        peers &= one ? ones : ~ones;
+    }
+    return peers;
+}
+
+// Rank of this lane's entry among the wavefront's entries of its digit so far, whose counters are moved on.
+__device__ __forceinline__ uint32_t rank_in_wave(volatile uint32_t* counter, uint32_t digit, int bits, bool there)
+{
+    const uint64_t peers = same_digit(digit, bits, there);
+    const uint32_t lane = __lane_id();
+    const uint32_t before = __popcll(peers & ((1ull << lane) - 1));
+    uint32_t rank = 0;
+    if (there) rank = counter[digit] + before;
+    __builtin_amdgcn_wave_barrier();                     // every lane has read before one of them writes
+    if (there && before == 0) counter[digit] = rank + __popcll(peers);
+    __builtin_amdgcn_wave_barrier();
+    return rank;
+}
+
+// Exclusive prefix over the block's threads; `sums` has one word for each wavefront.
+template <int WAVES>
+__device__ __forceinline__ uint32_t block_prefix(uint32_t x, uint32_t* sums)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t run = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t y = __shfl_up(run, o);
+        if (lane >= o) run += y;
+    }
+    if (lane == 63) sums[wave] = run;
+    __syncthreads();
+    uint32_t before = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) before += w < wave ? sums[w] : 0;
+    __syncthreads();
+    return before + run - x;
+}
+
+// ---- one workgroup -----------------------------------------------------------------------------------------------------
+
+template <int ITEMS>
+__global__ __launch_bounds__(kSmallBlock) void k_sort_small(const int32_t* __restrict__ index, int32_t m, uint32_t n_rows, int bits, int passes,
+                                                            int32_t* __restrict__ order, int32_t* __restrict__ place, int32_t* __restrict__ bounds,
+                                                            uint32_t* __restrict__ keys_out)
+{
+    constexpr int kW = kSmallBlock / 64;
+    __shared__ uint32_t keys[ITEMS * kSmallBlock], from[ITEMS * kSmallBlock];
+    __shared__ uint32_t counter[kW][1 << kMaxBits];
+    __shared__ uint32_t sums[kW];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int digits = 1 << bits;
+    uint32_t key[ITEMS], at[ITEMS];
+    // (a wavefront's entries are one run of ITEMS x 64, taken 64 at a time: their order is that of the ranks)
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int e = (wave * ITEMS + i) * 64 + lane;
+        at[i] = e;
+        key[i] = e < m ? key_of(index[e], n_rows) : 0;
+    }
+    for (int pass = 0; pass < passes; ++pass) {
+        for (int d = lane; d < digits; d += 64) counter[wave][d] = 0;
+        __builtin_amdgcn_wave_barrier();
+        uint32_t rank[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int e = (wave * ITEMS + i) * 64 + lane;
+            rank[i] = rank_in_wave(counter[wave], (key[i] >> (pass * bits)) & (digits - 1), bits, e < m);
+        }
+        __syncthreads();
+        uint32_t count = 0;                                  // digits <= block
+        if (tid < digits)
+            for (int w = 0; w < kW; ++w) count += counter[w][tid];
+        uint32_t start = block_prefix<kW>(count, sums);
+        if (tid < digits)
+            for (int w = 0; w < kW; ++w) {
+                const uint32_t n = counter[w][tid];
+                counter[w][tid] = start;
+                start += n;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int e = (wave * ITEMS + i) * 64 + lane;
+            if (e < m) {
+                const uint32_t to = counter[wave][(key[i] >> (pass * bits)) & (digits - 1)] + rank[i];
+                keys[to] = key[i];
+                from[to] = at[i];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int e = (wave * ITEMS + i) * 64 + lane;
+            if (e < m) {
+                key[i] = keys[e];
+                at[i] = from[e];
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int e = (wave * ITEMS + i) * 64 + lane;
+        if (e < m) {
+            order[e] = at[i];
+            if (place) place[at[i]] = key[i] < n_rows ? e : -1;
+            if (keys_out) keys_out[e] = key[i];
+        }
+    }
+    if (keys_out) return;                                    // many rows: k_sort_bounds
+    for (uint32_t v = tid; v <= n_rows; v += kSmallBlock) {
+        int lo = 0, hi = m;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (keys[mid] < v) lo = mid + 1; else hi = mid;
+        }
+        bounds[v] = lo;
+    }
+}
+
+// bounds[v]: entries whose key is below v
+__global__ __launch_bounds__(kBlock) void k_sort_bounds(const uint32_t* __restrict__ keys, int32_t m, int64_t n_rows, int32_t* __restrict__ bounds)
+{
+    const int64_t v = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (v > n_rows) return;
+    int64_t lo = 0, hi = m;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (keys[mid] < (uint32_t)v) lo = mid + 1; else hi = mid;
+    }
+    bounds[v] = (int32_t)lo;
+}
+
+// ---- many workgroups, one digit a pass ---------------------------------------------------------------------------------
+
+template <int ITEMS>
+__global__ __launch_bounds__(kBlock) void k_sort_count(const uint32_t* __restrict__ keys, int64_t m, uint32_t n_rows, int shift, int bits, int64_t tiles,
+                                                       uint32_t* __restrict__ counts)
+{
+    __shared__ uint32_t counter[1 << kMaxBits];
+    const int digits = 1 << bits;
+    for (int d = threadIdx.x; d < digits; d += kBlock) counter[d] = 0;
+    __syncthreads();
+    const int64_t first = (int64_t)blockIdx.x * (kBlock * ITEMS);
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int64_t e = first + i * kBlock + threadIdx.x;
+        if (e < m) atomicAdd(&counter[(key_of((int32_t)keys[e], n_rows) >> shift) & (digits - 1)], 1u);
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < digits; d += kBlock) counts[(int64_t)d * tiles + blockIdx.x] = counter[d];
+}
+
+// One workgroup a digit: exclusive prefix over the tiles, and the sum.
+__global__ __launch_bounds__(kBlock) void k_sort_scan(uint32_t* __restrict__ counts, int64_t tiles, uint32_t* __restrict__ totals)
+{
+    __shared__ uint32_t sums[kWaves];
+    __shared__ uint32_t carry;
+    uint32_t* row = counts + (int64_t)blockIdx.x * tiles;
+    uint32_t before = 0;
+    for (int64_t t0 = 0; t0 < tiles; t0 += kBlock) {
+        const int64_t t = t0 + threadIdx.x;
+        const uint32_t n = t < tiles ? row[t] : 0;
+        const uint32_t start = block_prefix<kWaves>(n, sums);
+        if (t < tiles) row[t] = before + start;
+        if (threadIdx.x == kBlock - 1) carry = start + n;
+        __syncthreads();
+        before += carry;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) totals[blockIdx.x] = before;
+}
+
+// FIRST: keys are the index itself and entries are numbered as they come.  LAST: place is written, with one pass in all the bounds too.
+template <int ITEMS, bool FIRST, bool LAST>
+__global__ __launch_bounds__(kBlock) void k_sort_scatter(const uint32_t* __restrict__ keys, const int32_t* __restrict__ from, int64_t m, uint32_t n_rows,
+                                                         int shift, int bits, int64_t tiles, const uint32_t* __restrict__ counts,
+                                                         const uint32_t* __restrict__ totals, uint32_t* __restrict__ keys_out,
+                                                         int32_t* __restrict__ order, int32_t* __restrict__ place, int32_t* __restrict__ bounds)
+{
+    __shared__ uint32_t counter[kWaves][1 << kMaxBits];
+    __shared__ uint32_t sums[kWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int digits = 1 << bits;
+    for (int d = lane; d < digits; d += 64) counter[wave][d] = 0;
+    __builtin_amdgcn_wave_barrier();
+    const int64_t first = (int64_t)blockIdx.x * (kBlock * ITEMS) + wave * (64 * ITEMS);
+    uint32_t key[ITEMS], rank[ITEMS];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int64_t e = first + i * 64 + lane;
+        key[i] = e < m ? (FIRST ? key_of((int32_t)keys[e], n_rows) : keys[e]) : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+        rank[i] = rank_in_wave(counter[wave], (key[i] >> shift) & (digits - 1), bits, first + i * 64 + lane < m);
+    __syncthreads();
+    uint32_t before = 0;
+    for (int d0 = 0; d0 < digits; d0 += kBlock) {
+        const int d = d0 + tid;
+        const uint32_t total = d < digits ? totals[d] : 0;
+        const uint32_t start = before + block_prefix<kWaves>(total, sums);
+        if (d < digits) {
+            if (bounds && blockIdx.x == 0 && d <= (int64_t)n_rows) bounds[d] = (int32_t)start;
+            uint32_t to = start + counts[(int64_t)d * tiles + blockIdx.x];
+            for (int w = 0; w < kWaves; ++w) {
+                const uint32_t n = counter[w][d];
+                counter[w][d] = to;
+                to += n;
+            }
+        }
+        if (tid == kBlock - 1) sums[0] = start + total;
+        __syncthreads();
+        before = sums[0];
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int64_t e = first + i * 64 + lane;
+        if (e < m) {
+            const uint32_t to = counter[wave][(key[i] >> shift) & (digits - 1)] + rank[i];
+            const int32_t entry = FIRST ? (int32_t)e : from[e];
+            order[to] = entry;
+            if (keys_out) keys_out[to] = key[i];
+            if (LAST && place) place[entry] = key[i] < n_rows ? (int32_t)to : -1;
+        }
+    }
+}
+
+template <int ITEMS>
+hipError_t many(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, int32_t* order, int32_t* place, int32_t* bounds, char* ws,
+                hipStream_t stream)
+{
+    const Layout l = layout_for(m, p);
+    uint32_t *counts = (uint32_t*)(ws + l.counts), *totals = (uint32_t*)(ws + l.totals);
+    uint32_t* key_to[2] = {(uint32_t*)(ws + l.key_a), (uint32_t*)(ws + l.key_b)};
+    int32_t* order_to[2] = {(int32_t*)(ws + l.order_a), (int32_t*)(ws + l.order_b)};
+    const uint32_t* keys = (const uint32_t*)index;
+    const int32_t* from = nullptr;
+    const unsigned tiles = (unsigned)p.tiles;
+    for (int pass = 0; pass < p.passes; ++pass) {
+        const bool first = pass == 0, last = pass == p.passes - 1;
+        const int shift = pass * p.bits;
+        uint32_t* keys_out = p.passes > 1 ? key_to[pass & 1] : nullptr;
+        int32_t* out = last ? order : order_to[pass & 1];
+        int32_t* starts = p.passes == 1 ? bounds : nullptr;
+        FG_LAUNCH(k_sort_count<ITEMS>, dim3(tiles), dim3(kBlock), 0, stream, keys, m, (uint32_t)n_rows, shift, p.bits, p.tiles, counts);
+        FG_LAUNCH(k_sort_scan, dim3(1u << p.bits), dim3(kBlock), 0, stream, counts, p.tiles, totals);
+        if (first && last)
+            FG_LAUNCH((k_sort_scatter<ITEMS, true, true>), dim3(tiles), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
+                      counts, totals, keys_out, out, place, starts);
+        else if (first)
+            FG_LAUNCH((k_sort_scatter<ITEMS, true, false>), dim3(tiles), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
+                      counts, totals, keys_out, out, place, starts);
+        else if (last)
+            FG_LAUNCH((k_sort_scatter<ITEMS, false, true>), dim3(tiles), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
+                      counts, totals, keys_out, out, place, starts);
+        else
+            FG_LAUNCH((k_sort_scatter<ITEMS, false, false>), dim3(tiles), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
+                      counts, totals, keys_out, out, place, starts);
+        keys = keys_out;
+        from = out;
+    }
+    if (p.passes > 1)
+        FG_LAUNCH(k_sort_bounds, dim3((unsigned)(n_rows / kBlock + 1)), dim3(kBlock), 0, stream, keys, (int32_t)m, n_rows, bounds);
+    return hipSuccess;
+}
+
+template <int ITEMS>
+hipError_t small(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, int32_t* order, int32_t* place, int32_t* bounds, void* workspace,
+                 hipStream_t stream)
+{
+    uint32_t* keys = n_rows > kSmallRows ? (uint32_t*)workspace : nullptr;
+    FG_LAUNCH(k_sort_small<ITEMS>, dim3(1), dim3(kSmallBlock), 0, stream, index, (int32_t)m, (uint32_t)n_rows, p.bits, p.passes, order, place, bounds, keys);
+    if (keys) FG_LAUNCH(k_sort_bounds, dim3((unsigned)(n_rows / kBlock + 1)), dim3(kBlock), 0, stream, keys, (int32_t)m, n_rows, bounds);
+    return hipSuccess;
+}
+
+}  // namespace
+
+size_t index_sort_workspace_bytes(int64_t m, int64_t n_rows)
+{
+    if (takes_small_sort(m)) return n_rows > kSmallRows ? up((size_t)m * 4) : 0;
+    return layout_for(m, plan_for(m, n_rows)).total;
+}
+
+hipError_t launch_index_sort(const int32_t* index, int64_t m, int64_t n_rows, int32_t* order, int32_t* place, int32_t* bounds, void* workspace,
+                             hipStream_t stream)
+{
+    const Plan p = plan_for(m, n_rows);
+    if (takes_small_sort(m)) {
+        if (m <= kSmallBlock) return small<1>(index, m, n_rows, p, order, place, bounds, workspace, stream);
+        if (m <= 2 * kSmallBlock) return small<2>(index, m, n_rows, p, order, place, bounds, workspace, stream);
+        return small<8>(index, m, n_rows, p, order, place, bounds, workspace, stream);
+    }
+    if (p.items == 4) return many<4>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);
+    return many<16>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);
+}
+
+}  // namespace fg
