@@ -269,7 +269,7 @@ typedef enum {
     FG_F16 = 2,
     FG_TYPE_INT_RANGE = 0x7fffffff
 } fg_type;
-#define FG_MAX_C (1 << 24)
+#define FG_MAX_C (1 << 18)
 #define FG_MAX_STRIDE (1 << 29)
 
 /* Stable counting sort of an index by the row that it names (what fg_bin_points does for points and bins).

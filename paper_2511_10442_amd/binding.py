@@ -450,7 +450,8 @@ def _weights(t, shape, device, name: str) -> int:
 
 def _call(name: str, device, *args):
     """The library's call on the device's current stream, with that device current."""
-    stream = torch.cuda.current_stream(device).cuda_stream
+    # (the stream as a number: a torch.cuda.Stream object takes longer to make than a small kernel to run)
+    stream = torch._C._cuda_getCurrentRawStream(device.index)
     if device.index == torch.cuda.current_device():
         _check(getattr(lib(), name)(*args, stream), name)
     else:
@@ -488,14 +489,37 @@ def fg_combine_backward_workspace_size(t: int, k: int, c: int, dtype: torch.dtyp
     return _sizes("fg_combine_backward_workspace_size", t, k, c, _TYPES[dtype])
 
 
-@dataclass
 class IndexSort:
     """An index in the order of the rows that it names (fg_index_sort)."""
-    index: torch.Tensor         # as it was given
-    n_rows: int
-    order: torch.Tensor         # [m] entries by row, ascending inside a row; those that name no row last
-    bounds: torch.Tensor        # [n_rows + 1] positions of the rows
-    place: torch.Tensor | None  # shape of the index: position of every entry, -1 where it names no row
+    __slots__ = ("index", "n_rows", "_words", "_place", "_views")
+
+    def __init__(self, index: torch.Tensor, n_rows: int, words: torch.Tensor, place: bool):
+        self.index, self.n_rows, self._words, self._place, self._views = index, n_rows, words, place, {}
+
+    def _view(self, name: str, first: int, count: int):
+        if name not in self._views:
+            self._views[name] = self._words[first:first + count]
+        return self._views[name]
+
+    @property
+    def order(self) -> torch.Tensor:
+        """[m] entries by row, ascending inside a row; those that name no row last."""
+        return self._view("order", 0, self.index.numel())
+
+    @property
+    def bounds(self) -> torch.Tensor:
+        """[n_rows + 1] positions of the rows."""
+        return self._view("bounds", self.index.numel(), self.n_rows + 1)
+
+    @property
+    def place(self) -> torch.Tensor | None:
+        """Shape of the index: position of every entry, -1 where it names no row.  None if it was not asked for."""
+        if not self._place:
+            return None
+        if "place" not in self._views:
+            m = self.index.numel()
+            self._views["place"] = self._words[m + self.n_rows + 1:].view(self.index.shape)
+        return self._views["place"]
 
 
 def fg_index_sort(index: torch.Tensor, n_rows: int, place: bool = True, workspace: torch.Tensor | None = None) -> IndexSort:
@@ -504,11 +528,10 @@ def fg_index_sort(index: torch.Tensor, n_rows: int, place: bool = True, workspac
     ptr = _index(index, "index", dev)
     m = index.numel()
     ws = _scratch(workspace, fg_index_sort_workspace_size(m, n_rows), dev)
-    order = torch.empty(m, dtype=torch.int32, device=dev)
-    bounds = torch.empty(n_rows + 1, dtype=torch.int32, device=dev)
-    at = torch.empty(index.shape, dtype=torch.int32, device=dev) if place else None
-    _call("fg_index_sort", dev, ptr, m, n_rows, _ptr(order), _ptr(at), _ptr(bounds), _ptr(ws), _bytes(ws))
-    return IndexSort(index, n_rows, order, bounds, at)
+    words = index.new_empty((2 * m if place else m) + n_rows + 1)        # order, bounds, place
+    at = words.data_ptr()
+    _call("fg_index_sort", dev, ptr, m, n_rows, at, at + 4 * (m + n_rows + 1) if place else None, at + 4 * m, _ptr(ws), _bytes(ws))
+    return IndexSort(index, n_rows, words, place)
 
 
 def fg_lookup(table: torch.Tensor, index: torch.Tensor, scale: float = 1.0, out: torch.Tensor | None = None) -> torch.Tensor:
@@ -517,12 +540,13 @@ def fg_lookup(table: torch.Tensor, index: torch.Tensor, scale: float = 1.0, out:
     rows, stride = _row_view(table, "table")
     names = _index(index, "index", dev)
     m, c = index.numel(), table.shape[1]
-    given = out
     if out is None:
-        out = torch.empty((m, c), dtype=table.dtype, device=dev)
-    to, to_stride = _row_view(out, "out", table.dtype, dev, (m, c))
+        out = table.new_empty((*index.shape, c))
+        to, to_stride = _ptr(out), c
+    else:
+        to, to_stride = _row_view(out, "out", table.dtype, dev, (m, c))
     _call("fg_lookup", dev, rows, _TYPES[table.dtype], table.shape[0], c, stride, names, m, scale, to, to_stride)
-    return out if given is not None or index.dim() == 1 else out.view(*index.shape, c)
+    return out
 
 
 def fg_lookup_backward(grad_out: torch.Tensor, sort: IndexSort, scale: float = 1.0, grad_table: torch.Tensor | None = None,
@@ -544,7 +568,7 @@ def fg_lookup_backward(grad_out: torch.Tensor, sort: IndexSort, scale: float = 1
         grad_table = torch.empty((sort.n_rows, c), dtype=dtype or grad_out.dtype, device=dev)
     to, to_stride = _row_view(grad_table, "grad_table", dtype, dev, (sort.n_rows, c))
     ws = _scratch(workspace, fg_lookup_backward_workspace_size(m, c, grad_out.dtype), dev)
-    _call("fg_lookup_backward", dev, grad, _TYPES[grad_out.dtype], m, c, stride, index, _ptr(sort.order), _ptr(sort.bounds), sort.n_rows, scale,
+    _call("fg_lookup_backward", dev, grad, _TYPES[grad_out.dtype], m, c, stride, index, sort._words.data_ptr(), sort._words.data_ptr() + 4 * m, sort.n_rows, scale,
           1 if accumulate else 0, to, _TYPES[grad_table.dtype], to_stride, _ptr(ws), _bytes(ws))
     return grad_table
 
@@ -575,8 +599,10 @@ def fg_combine(rows: torch.Tensor, index: torch.Tensor, weights: torch.Tensor | 
     t, k = index.shape
     n, c = rows.shape
     if out is None:
-        out = torch.empty((t, c), dtype=rows.dtype, device=dev)
-    to, to_stride = _row_view(out, "out", rows.dtype, dev, (t, c))
+        out = rows.new_empty((t, c))
+        to, to_stride = _ptr(out), c
+    else:
+        to, to_stride = _row_view(out, "out", rows.dtype, dev, (t, c))
     _call("fg_combine", dev, at, _TYPES[rows.dtype], n, c, stride, names, w, t, k, to, to_stride)
     return out
 
@@ -593,11 +619,12 @@ def fg_combine_backward(grad_out: torch.Tensor, rows: torch.Tensor, index: torch
     t, k = index.shape
     grad, grad_stride = _row_view(grad_out, "grad_out", rows.dtype, dev, (t, c))
     w = _weights(weights, index.shape, dev, "weights")
-    order = bounds = size = 0
+    order, bounds, size = None, None, 0
     if sort is not None:
         if sort.n_rows != n or sort.index.shape != index.shape or sort.index.device != dev:
             raise ValueError("sort must be fg_index_sort's of index for %d rows" % n)
-        order, bounds = _ptr(sort.order), _ptr(sort.bounds)
+        order = sort._words.data_ptr()
+        bounds = order + 4 * t * k
         size = fg_combine_backward_workspace_size(t, k, c, rows.dtype)
     if grad_rows is None:
         grad_rows = (torch.zeros if sort is None else torch.empty)((n, c), dtype=rows.dtype, device=dev)

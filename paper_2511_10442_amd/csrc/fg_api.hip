@@ -653,7 +653,7 @@ fg_status fg_combine_backward(const void* grad_out, int32_t type, int64_t t, int
     if (t > 0 && (!grad_out || !index || (grad_weights && !rows && n_rows > 0))) return FG_ERR_NULL;
     if (shared && (!bounds || (t > 0 && !order))) return FG_ERR_NULL;
     if (misaligned(type, {grad_out, rows, grad_rows})) return FG_ERR_UNSUPPORTED;
-    const bool sums = shared && grad_rows && n_rows > 0;
+    const bool sums = shared && grad_rows && n_rows > 0, products = sums && t > 0 && grad_weights && sums_with_products(type, c);
     if (sums && bad_workspace(workspace, workspace_bytes, row_sums_workspace_bytes(type, t * k, c))) return FG_ERR_WORKSPACE;
     if (sums) {
         RowSums a = {};
@@ -661,11 +661,12 @@ fg_status fg_combine_backward(const void* grad_out, int32_t type, int64_t t, int
         a.grad = {grad_out, grad_stride}; a.out = {grad_rows, grad_rows_stride};
         a.index = index; a.order = order; a.bounds = bounds; a.weights = weights;
         a.m = t * k; a.n_rows = n_rows; a.c = c; a.fan = k; a.scale = 1.0f;
+        if (products) { a.rows = {rows, rows_stride}; a.grad_weights = grad_weights; }
         a.partials = (float*)workspace;
         if (launch_row_sums(a, (hipStream_t)stream) != hipSuccess) return FG_ERR_LAUNCH;
     }
     void* once = shared ? nullptr : grad_rows;
-    if (t == 0 || (!once && !grad_weights)) return FG_OK;
+    if (t == 0 || products || (!once && !grad_weights)) return FG_OK;
     return told(launch_combine_grad(type, {grad_out, grad_stride}, t, c, {rows, rows_stride}, n_rows, index, weights, k,
                                     {once, grad_rows_stride}, grad_weights, (hipStream_t)stream));
 }

@@ -16,6 +16,7 @@ constexpr int64_t kSmallM = 8192;            // entries that one workgroup sorts
 constexpr int64_t kSmallRows = 4096;         // rows whose bounds that workgroup writes too
 constexpr int kBlock = 256;
 constexpr int kWaves = kBlock / 64;
+constexpr unsigned kXcds = 8;
 
 struct Plan { int bits, passes, items; int64_t tiles; };
 
@@ -80,19 +81,19 @@ __device__ __forceinline__ uint32_t rank_in_wave(volatile uint32_t* counter, uin
 }
 
 // Exclusive prefix over the block's threads; `sums` has one word for each wavefront.
-template <int WAVES>
-__device__ __forceinline__ uint32_t block_prefix(uint32_t x, uint32_t* sums)
+template <int WAVES, typename W>
+__device__ __forceinline__ W block_prefix(W x, W* sums)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t run = x;
+    W run = x;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t y = __shfl_up(run, o);
+        const W y = __shfl_up(run, o);
         if (lane >= o) run += y;
     }
     if (lane == 63) sums[wave] = run;
     __syncthreads();
-    uint32_t before = 0;
+    W before = 0;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) before += w < wave ? sums[w] : 0;
     __syncthreads();
@@ -233,6 +234,8 @@ __global__ __launch_bounds__(kBlock) void k_sort_scan(uint32_t* __restrict__ cou
     if (threadIdx.x == 0) totals[blockIdx.x] = before;
 }
 
+// A tile is put in order in LDS first, so that its entries of one digit leave as one run; runs of neighbouring tiles lie next to each other, and
+// neighbouring tiles are workgroups of one XCD, whose L2 joins them into whole lines.
 // FIRST: keys are the index itself and entries are numbered as they come.  LAST: place is written, with one pass in all the bounds too.
 template <int ITEMS, bool FIRST, bool LAST>
 __global__ __launch_bounds__(kBlock) void k_sort_scatter(const uint32_t* __restrict__ keys, const int32_t* __restrict__ from, int64_t m, uint32_t n_rows,
@@ -240,51 +243,72 @@ __global__ __launch_bounds__(kBlock) void k_sort_scatter(const uint32_t* __restr
                                                          const uint32_t* __restrict__ totals, uint32_t* __restrict__ keys_out,
                                                          int32_t* __restrict__ order, int32_t* __restrict__ place, int32_t* __restrict__ bounds)
 {
+    constexpr int kTile = kBlock * ITEMS;
     __shared__ uint32_t counter[kWaves][1 << kMaxBits];
-    __shared__ uint32_t sums[kWaves];
+    __shared__ uint32_t away[1 << kMaxBits];             // of a digit: from its place in the tile to its place in the order
+    __shared__ uint32_t sorted[kTile];
+    __shared__ int32_t entries[kTile];
+    __shared__ uint64_t sums[kWaves];
+    const int64_t tile = (int64_t)(blockIdx.x % kXcds) * (gridDim.x / kXcds) + blockIdx.x / kXcds;
+    if (tile >= tiles) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int digits = 1 << bits;
     for (int d = lane; d < digits; d += 64) counter[wave][d] = 0;
     __builtin_amdgcn_wave_barrier();
-    const int64_t first = (int64_t)blockIdx.x * (kBlock * ITEMS) + wave * (64 * ITEMS);
+    const int64_t first = tile * kTile + wave * (64 * ITEMS);
     uint32_t key[ITEMS], rank[ITEMS];
+    int32_t entry[ITEMS];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         const int64_t e = first + i * 64 + lane;
         key[i] = e < m ? (FIRST ? key_of((int32_t)keys[e], n_rows) : keys[e]) : 0;
+        entry[i] = FIRST || e >= m ? (int32_t)e : from[e];
     }
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
         rank[i] = rank_in_wave(counter[wave], (key[i] >> shift) & (digits - 1), bits, first + i * 64 + lane < m);
     __syncthreads();
-    uint32_t before = 0;
+    uint64_t before = 0;                                 // of the whole order in the upper half, of the tile in the lower
     for (int d0 = 0; d0 < digits; d0 += kBlock) {
         const int d = d0 + tid;
-        const uint32_t total = d < digits ? totals[d] : 0;
-        const uint32_t start = before + block_prefix<kWaves>(total, sums);
+        uint32_t here = 0;
+        if (d < digits)
+            for (int w = 0; w < kWaves; ++w) here += counter[w][d];
+        const uint64_t both = d < digits ? (uint64_t)totals[d] << 32 | here : 0;
+        const uint64_t start = before + block_prefix<kWaves>(both, sums);
         if (d < digits) {
-            if (bounds && blockIdx.x == 0 && d <= (int64_t)n_rows) bounds[d] = (int32_t)start;
-            uint32_t to = start + counts[(int64_t)d * tiles + blockIdx.x];
+            const uint32_t all = (uint32_t)(start >> 32);
+            uint32_t to = (uint32_t)start;
+            if (bounds && tile == 0 && d <= (int64_t)n_rows) bounds[d] = (int32_t)all;
+            away[d] = all + counts[(int64_t)d * tiles + tile] - to;
             for (int w = 0; w < kWaves; ++w) {
                 const uint32_t n = counter[w][d];
                 counter[w][d] = to;
                 to += n;
             }
         }
-        if (tid == kBlock - 1) sums[0] = start + total;
+        if (tid == kBlock - 1) sums[0] = start + both;
         __syncthreads();
         before = sums[0];
         __syncthreads();
     }
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        const int64_t e = first + i * 64 + lane;
-        if (e < m) {
+    for (int i = 0; i < ITEMS; ++i)
+        if (first + i * 64 + lane < m) {
             const uint32_t to = counter[wave][(key[i] >> shift) & (digits - 1)] + rank[i];
-            const int32_t entry = FIRST ? (int32_t)e : from[e];
-            order[to] = entry;
-            if (keys_out) keys_out[to] = key[i];
-            if (LAST && place) place[entry] = key[i] < n_rows ? (int32_t)to : -1;
+            sorted[to] = key[i];
+            entries[to] = entry[i];
+        }
+    __syncthreads();
+    const int64_t left = m - tile * kTile;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int p = i * kBlock + tid;
+        if (p < left) {
+            const uint32_t k = sorted[p], to = away[(k >> shift) & (digits - 1)] + p;
+            order[to] = entries[p];
+            if (keys_out) keys_out[to] = k;
+            if (LAST && place) place[entries[p]] = k < n_rows ? (int32_t)to : -1;
         }
     }
 }
@@ -299,7 +323,7 @@ hipError_t many(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, 
     int32_t* order_to[2] = {(int32_t*)(ws + l.order_a), (int32_t*)(ws + l.order_b)};
     const uint32_t* keys = (const uint32_t*)index;
     const int32_t* from = nullptr;
-    const unsigned tiles = (unsigned)p.tiles;
+    const unsigned tiles = (unsigned)p.tiles, spread = (tiles + kXcds - 1) / kXcds * kXcds;
     for (int pass = 0; pass < p.passes; ++pass) {
         const bool first = pass == 0, last = pass == p.passes - 1;
         const int shift = pass * p.bits;
@@ -309,16 +333,16 @@ hipError_t many(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, 
         FG_LAUNCH(k_sort_count<ITEMS>, dim3(tiles), dim3(kBlock), 0, stream, keys, m, (uint32_t)n_rows, shift, p.bits, p.tiles, counts);
         FG_LAUNCH(k_sort_scan, dim3(1u << p.bits), dim3(kBlock), 0, stream, counts, p.tiles, totals);
         if (first && last)
-            FG_LAUNCH((k_sort_scatter<ITEMS, true, true>), dim3(tiles), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
+            FG_LAUNCH((k_sort_scatter<ITEMS, true, true>), dim3(spread), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
                       counts, totals, keys_out, out, place, starts);
         else if (first)
-            FG_LAUNCH((k_sort_scatter<ITEMS, true, false>), dim3(tiles), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
+            FG_LAUNCH((k_sort_scatter<ITEMS, true, false>), dim3(spread), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
                       counts, totals, keys_out, out, place, starts);
         else if (last)
-            FG_LAUNCH((k_sort_scatter<ITEMS, false, true>), dim3(tiles), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
+            FG_LAUNCH((k_sort_scatter<ITEMS, false, true>), dim3(spread), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
                       counts, totals, keys_out, out, place, starts);
         else
-            FG_LAUNCH((k_sort_scatter<ITEMS, false, false>), dim3(tiles), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
+            FG_LAUNCH((k_sort_scatter<ITEMS, false, false>), dim3(spread), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
                       counts, totals, keys_out, out, place, starts);
         keys = keys_out;
         from = out;

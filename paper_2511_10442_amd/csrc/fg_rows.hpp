@@ -45,12 +45,16 @@ struct RowSums {
     RowsOut out;
     const int32_t *index, *order, *bounds;
     const float* weights;
+    RowsIn rows;             // with grad_weights (sums_with_products): the rows that the entries name
+    float* grad_weights;     // or NULL
     int64_t m, n_rows, c;
     int32_t fan;
     float scale;
     int32_t accumulate;
     float* partials;     // row_sums_workspace_bytes()
 };
+// Widths of rows whose products with the summed rows, the weights' gradient, are made along with the sums.
+bool sums_with_products(int32_t type, int64_t c);
 size_t row_sums_workspace_bytes(int32_t type, int64_t m, int64_t c);
 hipError_t launch_row_sums(const RowSums& a, hipStream_t stream);
 

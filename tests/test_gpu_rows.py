@@ -302,6 +302,26 @@ def test_messages_from_neighbours(n, k, c, dtype):
     R.check(alone, ref, mass, count[:, None], dtype)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,t,k,c", [(5, 300, 7, 24), (3, 1500, 16, 8), (4, 9000, 8, 200), (2500, 4000, 30, 256), (90, 700, 5, 512), (60, 500, 5, 520), (40000, 90000, 3, 5)])
+def test_shared_rows(n, t, k, c, dtype):
+    """Rows named by few and by thousands of entries, with lanes of a row that have no piece, and rows too wide for products along the way"""
+    rng = np.random.default_rng(n + t)
+    index = some_index(rng, (t, k), n, "frequent")
+    rows, grad, w = values(rng, n, c, dtype), values(rng, t, c, dtype), dev(rng.random((t, k)).astype(np.float32))
+    by = B.fg_index_sort(dev(index), n)
+    for weights in (w, None):
+        wide = None if weights is None else R.wide(w)
+        gw = torch.full((t, k), 7.0, device=DEV)
+        got, gw = B.fg_combine_backward(grad, rows, dev(index), weights, sort=by, grad_weights=gw)
+        ref, mass, count = R.row_sums(R.wide(grad), index, wide, n)
+        R.check(got, ref, mass, count[:, None], dtype)
+        R.check(gw, *R.dots(R.wide(grad), R.wide(rows), index), c, torch.float32)
+        assert torch.equal(got, B.fg_combine_backward(grad, rows, dev(index), weights, sort=by)[0])
+    ref, mass = R.combine(R.wide(rows), index, R.wide(w))
+    R.check(B.fg_combine(rows, dev(index), w), ref, mass, k, dtype)
+
+
 def test_gradients_against_differences():
     """Outputs are linear in rows and in weights: a step of 1 in one of them changes the loss by its gradient, but for rounding"""
     rng = np.random.default_rng(12)

@@ -42,7 +42,7 @@ def test_lookup(lib):
     ok = dict(table=256, type=BF16, n=5, c=8, ts=8, index=8, m=3, scale=1.0, out=512, os=8)
     call = lambda **k: f(*dict(ok, **k).values(), None)      # noqa: E731
     assert call(type=3) == call(type=-1) == B.FG_ERR_UNSUPPORTED
-    assert call(c=0) == call(c=-3) == call(c=(1 << 24) + 1) == B.FG_ERR_BAD_SHAPE
+    assert call(c=0) == call(c=-3) == call(c=(1 << 18) + 1) == B.FG_ERR_BAD_SHAPE
     assert call(ts=-8) == call(ts=(1 << 29) + 1) == call(os=7) == call(os=0) == call(os=(1 << 29) + 1) == B.FG_ERR_BAD_SHAPE
     assert call(m=-1) == call(m=N + 1) == call(n=-1) == call(n=N + 1) == B.FG_ERR_BAD_SHAPE
     assert call(table=None) == call(index=None) == call(out=None) == B.FG_ERR_NULL
@@ -103,7 +103,7 @@ def test_combine_backward(lib):
 
 def test_the_binding_refuses_tensors_that_are_not_on_a_device():
     i, x = torch.zeros((4, 2), dtype=torch.int32), torch.zeros((4, 8))
-    by = B.IndexSort(i, 4, i.reshape(-1), torch.zeros(5, dtype=torch.int32), i)
+    by = B.IndexSort(i, 4, torch.zeros(8 + 5 + 8, dtype=torch.int32), True)
     for call in (lambda: B.fg_index_sort(i, 4), lambda: B.fg_lookup(x, i), lambda: B.fg_lookup_backward(torch.zeros((8, 8)), by),
                  lambda: B.fg_dispatch(x, i), lambda: B.fg_combine(x, i), lambda: B.fg_combine_backward(x, x, i)):
         with pytest.raises(ValueError):
