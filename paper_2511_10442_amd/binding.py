@@ -7,6 +7,7 @@ CPU fallback: if the library has not been built this module raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 
@@ -419,44 +420,48 @@ def _row_view(t: torch.Tensor, name: str, dtype=None, device=None, shape=None):
         raise ValueError("%s must be a device tensor" % name)
     if t.dim() != 2 or (dtype is not None and t.dtype != dtype) or t.dtype not in _TYPES:
         raise ValueError("%s must be 2-d %s" % (name, dtype or "float32, bfloat16 or float16"))
-    n, c = t.shape
-    if shape is not None and (n, c) != shape:
-        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), (n, c)))
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
     if device is not None and t.device != device:
         raise ValueError("%s must be on %s" % (name, device))
+    n, c = t.shape
     stride, one = t.stride()
     if one != 1 and c > 1 and n > 0:
         raise ValueError("%s must have contiguous rows" % name)
-    return _ptr(t), (stride if n > 1 else c)
+    return t.data_ptr() or None, (stride if n > 1 else c)
 
 
-def _index(t: torch.Tensor, name: str, device, dims=None) -> int:
-    _dev(t, torch.int32, name)
+def _index(t: torch.Tensor, name: str, device, dims=None):
+    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 device tensor" % name)
     if t.device != device:
         raise ValueError("%s must be on %s" % (name, device))
     if dims is not None and t.dim() != dims:
         raise ValueError("%s must be %d-d" % (name, dims))
-    return _ptr(t)
+    return t.data_ptr() or None
 
 
-def _weights(t, shape, device, name: str) -> int:
+def _weights(t, shape, device, name: str):
     if t is None:
-        return 0
+        return None
     _dev(t, torch.float32, name)
     if t.shape != shape or t.device != device:
         raise ValueError("%s must have shape %s and be on %s" % (name, tuple(shape), device))
-    return _ptr(t)
+    return t.data_ptr() or None
 
 
 def _call(name: str, device, *args):
     """The library's call on the device's current stream, with that device current."""
     # (the stream as a number: a torch.cuda.Stream object takes longer to make than a small kernel to run)
-    stream = torch._C._cuda_getCurrentRawStream(device.index)
-    if device.index == torch.cuda.current_device():
-        _check(getattr(lib(), name)(*args, stream), name)
+    at = device.index
+    fn = getattr(_lib or lib(), name)
+    if at == torch.cuda.current_device():
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(at))
     else:
         with torch.cuda.device(device):
-            _check(getattr(lib(), name)(*args, stream), name)
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(at))
+    if status != FG_OK:
+        raise FgError(status, name)
 
 
 def _scratch(workspace, size: int, device):
@@ -471,6 +476,7 @@ def _bytes(t) -> int:
     return 0 if t is None else t.numel() * t.element_size()
 
 
+@functools.lru_cache(maxsize=4096)
 def _sizes(name: str, *args) -> int:
     out = ctypes.c_size_t(0)
     _check(getattr(lib(), name)(*args, ctypes.byref(out)), name)
@@ -518,7 +524,7 @@ class IndexSort:
             return None
         if "place" not in self._views:
             m = self.index.numel()
-            self._views["place"] = self._words[m + self.n_rows + 1:].view(self.index.shape)
+            self._views["place"] = self._words.as_strided(self.index.shape, self.index.stride(), m + self.n_rows + 1)
         return self._views["place"]
 
 
@@ -542,7 +548,7 @@ def fg_lookup(table: torch.Tensor, index: torch.Tensor, scale: float = 1.0, out:
     m, c = index.numel(), table.shape[1]
     if out is None:
         out = table.new_empty((*index.shape, c))
-        to, to_stride = _ptr(out), c
+        to, to_stride = out.data_ptr() or None, c
     else:
         to, to_stride = _row_view(out, "out", table.dtype, dev, (m, c))
     _call("fg_lookup", dev, rows, _TYPES[table.dtype], table.shape[0], c, stride, names, m, scale, to, to_stride)
@@ -600,7 +606,7 @@ def fg_combine(rows: torch.Tensor, index: torch.Tensor, weights: torch.Tensor | 
     n, c = rows.shape
     if out is None:
         out = rows.new_empty((t, c))
-        to, to_stride = _ptr(out), c
+        to, to_stride = out.data_ptr() or None, c
     else:
         to, to_stride = _row_view(out, "out", rows.dtype, dev, (t, c))
     _call("fg_combine", dev, at, _TYPES[rows.dtype], n, c, stride, names, w, t, k, to, to_stride)

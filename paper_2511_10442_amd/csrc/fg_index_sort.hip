@@ -15,10 +15,12 @@ constexpr int kSmallBlock = 1024;
 constexpr int64_t kSmallM = 8192;            // entries that one workgroup sorts in LDS
 constexpr int64_t kSmallRows = 4096;         // rows whose bounds that workgroup writes too
 constexpr int kBlock = 256;
-constexpr int kWaves = kBlock / 64;
 constexpr unsigned kXcds = 8;
+constexpr int kItems = 4;                    // a tile: kBlock x kItems entries, or beyond kMediumM
+constexpr int64_t kMediumM = 1 << 20;
+constexpr int kLargeBlock = 512, kLargeItems = 8;
 
-struct Plan { int bits, passes, items; int64_t tiles; };
+struct Plan { int bits, passes; bool large; int64_t tiles; };
 
 inline Plan plan_for(int64_t m, int64_t n_rows)
 {
@@ -27,8 +29,9 @@ inline Plan plan_for(int64_t m, int64_t n_rows)
     while (((int64_t)1 << bits) <= n_rows) ++bits;       // keys 0..n_rows
     p.passes = (bits + kMaxBits - 1) / kMaxBits;
     p.bits = (bits + p.passes - 1) / p.passes;
-    p.items = m <= (1 << 20) ? 4 : 16;
-    p.tiles = (m + (int64_t)kBlock * p.items - 1) / ((int64_t)kBlock * p.items);
+    p.large = m > kMediumM;
+    const int64_t tile = p.large ? kLargeBlock * kLargeItems : kBlock * kItems;
+    p.tiles = (m + tile - 1) / tile;
     return p;
 }
 
@@ -79,6 +82,9 @@ __device__ __forceinline__ uint32_t rank_in_wave(volatile uint32_t* counter, uin
     __builtin_amdgcn_wave_barrier();
     return rank;
 }
+
+// Neighbouring tiles are workgroups of one XCD, whose L2 joins what they write next to each other; the grid is a multiple of kXcds.
+__device__ __forceinline__ int64_t tile_of_block() { return (int64_t)(blockIdx.x % kXcds) * (gridDim.x / kXcds) + blockIdx.x / kXcds; }
 
 // Exclusive prefix over the block's threads; `sums` has one word for each wavefront.
 template <int WAVES, typename W>
@@ -181,42 +187,64 @@ __global__ __launch_bounds__(kSmallBlock) void k_sort_small(const int32_t* __res
     }
 }
 
-// bounds[v]: entries whose key is below v
+// bounds[v]: entries whose key is below v.  Fifteen places are looked at a time, which cost one trip to memory.
 __global__ __launch_bounds__(kBlock) void k_sort_bounds(const uint32_t* __restrict__ keys, int32_t m, int64_t n_rows, int32_t* __restrict__ bounds)
 {
     const int64_t v = (int64_t)blockIdx.x * kBlock + threadIdx.x;
     if (v > n_rows) return;
+    constexpr int kWays = 16;
     int64_t lo = 0, hi = m;
     while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (keys[mid] < (uint32_t)v) lo = mid + 1; else hi = mid;
+        const int64_t step = (hi - lo + kWays - 1) / kWays;
+        uint32_t key[kWays - 1];
+#pragma unroll
+        for (int i = 0; i < kWays - 1; ++i) {
+            const int64_t at = lo + (i + 1) * step - 1;
+            key[i] = keys[at < hi ? at : hi - 1];
+        }
+        int below = 0;
+#pragma unroll
+        for (int i = 0; i < kWays - 1; ++i) below += lo + (i + 1) * step - 1 < hi && key[i] < (uint32_t)v;
+        lo += below * step;
+        if (below < kWays - 1 && hi > lo + step - 1) hi = lo + step - 1;     // (the place looked at behind the last run would be hi itself)
     }
     bounds[v] = (int32_t)lo;
 }
 
 // ---- many workgroups, one digit a pass ---------------------------------------------------------------------------------
 
-template <int ITEMS>
-__global__ __launch_bounds__(kBlock) void k_sort_count(const uint32_t* __restrict__ keys, int64_t m, uint32_t n_rows, int shift, int bits, int64_t tiles,
-                                                       uint32_t* __restrict__ counts)
+template <int BLOCK, int ITEMS>
+__global__ __launch_bounds__(BLOCK) void k_sort_count(const uint32_t* __restrict__ keys, int64_t m, uint32_t n_rows, int shift, int bits, int64_t tiles,
+                                                      uint32_t* __restrict__ counts)
 {
+    typedef uint32_t Four __attribute__((ext_vector_type(4), aligned(4)));
     __shared__ uint32_t counter[1 << kMaxBits];
     const int digits = 1 << bits;
-    for (int d = threadIdx.x; d < digits; d += kBlock) counter[d] = 0;
+    const int64_t tile = tile_of_block();
+    if (tile >= tiles) return;
+    for (int d = threadIdx.x; d < digits; d += BLOCK) counter[d] = 0;
     __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * (kBlock * ITEMS);
+    const int64_t first = tile * (BLOCK * ITEMS);
+    auto add = [&](uint32_t key) { atomicAdd(&counter[(key_of((int32_t)key, n_rows) >> shift) & (digits - 1)], 1u); };
+    if (first + BLOCK * ITEMS <= m) {
+        Four v[ITEMS / 4];
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        const int64_t e = first + i * kBlock + threadIdx.x;
-        if (e < m) atomicAdd(&counter[(key_of((int32_t)keys[e], n_rows) >> shift) & (digits - 1)], 1u);
+        for (int i = 0; i < ITEMS / 4; ++i) v[i] = *reinterpret_cast<const Four*>(keys + first + (i * BLOCK + threadIdx.x) * 4);
+#pragma unroll
+        for (int i = 0; i < ITEMS / 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) add(v[i][j]);
+    } else {
+        for (int64_t e = first + threadIdx.x; e < m; e += BLOCK) add(keys[e]);
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < digits; d += kBlock) counts[(int64_t)d * tiles + blockIdx.x] = counter[d];
+    for (int d = threadIdx.x; d < digits; d += BLOCK) counts[(int64_t)d * tiles + tile] = counter[d];
 }
 
 // One workgroup a digit: exclusive prefix over the tiles, and the sum.
 __global__ __launch_bounds__(kBlock) void k_sort_scan(uint32_t* __restrict__ counts, int64_t tiles, uint32_t* __restrict__ totals)
 {
+    constexpr int kWaves = kBlock / 64;
     __shared__ uint32_t sums[kWaves];
     __shared__ uint32_t carry;
     uint32_t* row = counts + (int64_t)blockIdx.x * tiles;
@@ -234,27 +262,29 @@ __global__ __launch_bounds__(kBlock) void k_sort_scan(uint32_t* __restrict__ cou
     if (threadIdx.x == 0) totals[blockIdx.x] = before;
 }
 
-// A tile is put in order in LDS first, so that its entries of one digit leave as one run; runs of neighbouring tiles lie next to each other, and
-// neighbouring tiles are workgroups of one XCD, whose L2 joins them into whole lines.
+// A tile is put in order in LDS first, so that its entries of one digit leave as one run; runs of neighbouring tiles lie next to each other.
 // FIRST: keys are the index itself and entries are numbered as they come.  LAST: place is written, with one pass in all the bounds too.
-template <int ITEMS, bool FIRST, bool LAST>
-__global__ __launch_bounds__(kBlock) void k_sort_scatter(const uint32_t* __restrict__ keys, const int32_t* __restrict__ from, int64_t m, uint32_t n_rows,
-                                                         int shift, int bits, int64_t tiles, const uint32_t* __restrict__ counts,
-                                                         const uint32_t* __restrict__ totals, uint32_t* __restrict__ keys_out,
-                                                         int32_t* __restrict__ order, int32_t* __restrict__ place, int32_t* __restrict__ bounds)
+template <int BLOCK, int ITEMS>
+constexpr size_t scatter_lds(int digits) { return ((size_t)digits * (BLOCK / 64 + 1) + 2 * BLOCK * ITEMS) * 4; }
+
+template <int BLOCK, int ITEMS, bool FIRST, bool LAST>
+__global__ __launch_bounds__(BLOCK) void k_sort_scatter(const uint32_t* __restrict__ keys, const int32_t* __restrict__ from, int64_t m, uint32_t n_rows,
+                                                        int shift, int bits, int64_t tiles, const uint32_t* __restrict__ counts,
+                                                        const uint32_t* __restrict__ totals, uint32_t* __restrict__ keys_out,
+                                                        int32_t* __restrict__ order, int32_t* __restrict__ place, int32_t* __restrict__ bounds)
 {
-    constexpr int kTile = kBlock * ITEMS;
-    __shared__ uint32_t counter[kWaves][1 << kMaxBits];
-    __shared__ uint32_t away[1 << kMaxBits];             // of a digit: from its place in the tile to its place in the order
-    __shared__ uint32_t sorted[kTile];
-    __shared__ int32_t entries[kTile];
+    constexpr int kTile = BLOCK * ITEMS, kWaves = BLOCK / 64, kOwn = (1 << kMaxBits) / BLOCK;
+    extern __shared__ uint32_t lds[];                    // scatter_lds()
     __shared__ uint64_t sums[kWaves];
-    const int64_t tile = (int64_t)(blockIdx.x % kXcds) * (gridDim.x / kXcds) + blockIdx.x / kXcds;
+    const int digits = 1 << bits;
+    uint32_t* sorted = lds;
+    int32_t* entries = (int32_t*)(lds + kTile);
+    uint32_t* away = lds + 2 * kTile;                    // of a digit: from its place in the tile to its place in the order
+    uint32_t* counters = away + digits;                  // [wave][digit]
+    const int64_t tile = tile_of_block();
     if (tile >= tiles) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int digits = 1 << bits;
-    for (int d = lane; d < digits; d += 64) counter[wave][d] = 0;
-    __builtin_amdgcn_wave_barrier();
+    uint32_t* counter = counters + wave * digits;
     const int64_t first = tile * kTile + wave * (64 * ITEMS);
     uint32_t key[ITEMS], rank[ITEMS];
     int32_t entry[ITEMS];
@@ -264,30 +294,41 @@ __global__ __launch_bounds__(kBlock) void k_sort_scatter(const uint32_t* __restr
         key[i] = e < m ? (FIRST ? key_of((int32_t)keys[e], n_rows) : keys[e]) : 0;
         entry[i] = FIRST || e >= m ? (int32_t)e : from[e];
     }
+    uint32_t total[kOwn], already[kOwn];                 // of this lane's digits: in the index, in the tiles before
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+        const int d = i * BLOCK + tid;
+        total[i] = d < digits ? totals[d] : 0;
+        already[i] = d < digits ? counts[(int64_t)d * tiles + tile] : 0;
+    }
+    for (int d = lane; d < digits; d += 64) counter[d] = 0;
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
-        rank[i] = rank_in_wave(counter[wave], (key[i] >> shift) & (digits - 1), bits, first + i * 64 + lane < m);
+        rank[i] = rank_in_wave(counter, (key[i] >> shift) & (digits - 1), bits, first + i * 64 + lane < m);
     __syncthreads();
     uint64_t before = 0;                                 // of the whole order in the upper half, of the tile in the lower
-    for (int d0 = 0; d0 < digits; d0 += kBlock) {
-        const int d = d0 + tid;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+        if (i * BLOCK >= digits) break;
+        const int d = i * BLOCK + tid;
         uint32_t here = 0;
         if (d < digits)
-            for (int w = 0; w < kWaves; ++w) here += counter[w][d];
-        const uint64_t both = d < digits ? (uint64_t)totals[d] << 32 | here : 0;
+            for (int w = 0; w < kWaves; ++w) here += counters[w * digits + d];
+        const uint64_t both = (uint64_t)total[i] << 32 | here;
         const uint64_t start = before + block_prefix<kWaves>(both, sums);
         if (d < digits) {
             const uint32_t all = (uint32_t)(start >> 32);
             uint32_t to = (uint32_t)start;
             if (bounds && tile == 0 && d <= (int64_t)n_rows) bounds[d] = (int32_t)all;
-            away[d] = all + counts[(int64_t)d * tiles + tile] - to;
+            away[d] = all + already[i] - to;
             for (int w = 0; w < kWaves; ++w) {
-                const uint32_t n = counter[w][d];
-                counter[w][d] = to;
+                const uint32_t n = counters[w * digits + d];
+                counters[w * digits + d] = to;
                 to += n;
             }
         }
-        if (tid == kBlock - 1) sums[0] = start + both;
+        if (tid == BLOCK - 1) sums[0] = start + both;
         __syncthreads();
         before = sums[0];
         __syncthreads();
@@ -295,7 +336,7 @@ __global__ __launch_bounds__(kBlock) void k_sort_scatter(const uint32_t* __restr
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
         if (first + i * 64 + lane < m) {
-            const uint32_t to = counter[wave][(key[i] >> shift) & (digits - 1)] + rank[i];
+            const uint32_t to = counter[(key[i] >> shift) & (digits - 1)] + rank[i];
             sorted[to] = key[i];
             entries[to] = entry[i];
         }
@@ -303,7 +344,7 @@ __global__ __launch_bounds__(kBlock) void k_sort_scatter(const uint32_t* __restr
     const int64_t left = m - tile * kTile;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        const int p = i * kBlock + tid;
+        const int p = i * BLOCK + tid;
         if (p < left) {
             const uint32_t k = sorted[p], to = away[(k >> shift) & (digits - 1)] + p;
             order[to] = entries[p];
@@ -313,7 +354,18 @@ __global__ __launch_bounds__(kBlock) void k_sort_scatter(const uint32_t* __restr
     }
 }
 
-template <int ITEMS>
+template <int BLOCK, int ITEMS, bool FIRST, bool LAST, typename... Args>
+hipError_t scatter(unsigned blocks, int bits, hipStream_t stream, Args... args)
+{
+    const size_t lds = scatter_lds<BLOCK, ITEMS>(1 << bits);
+    // (beyond 64 KiB a kernel has to be told)
+    if (lds > 65536)
+        FG_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_sort_scatter<BLOCK, ITEMS, FIRST, LAST>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    FG_LAUNCH((k_sort_scatter<BLOCK, ITEMS, FIRST, LAST>), dim3(blocks), dim3(BLOCK), lds, stream, args...);
+    return hipSuccess;
+}
+
+template <int BLOCK, int ITEMS>
 hipError_t many(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, int32_t* order, int32_t* place, int32_t* bounds, char* ws,
                 hipStream_t stream)
 {
@@ -323,27 +375,23 @@ hipError_t many(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, 
     int32_t* order_to[2] = {(int32_t*)(ws + l.order_a), (int32_t*)(ws + l.order_b)};
     const uint32_t* keys = (const uint32_t*)index;
     const int32_t* from = nullptr;
-    const unsigned tiles = (unsigned)p.tiles, spread = (tiles + kXcds - 1) / kXcds * kXcds;
+    const unsigned spread = (unsigned)((p.tiles + kXcds - 1) / kXcds * kXcds);
     for (int pass = 0; pass < p.passes; ++pass) {
         const bool first = pass == 0, last = pass == p.passes - 1;
         const int shift = pass * p.bits;
         uint32_t* keys_out = p.passes > 1 ? key_to[pass & 1] : nullptr;
         int32_t* out = last ? order : order_to[pass & 1];
         int32_t* starts = p.passes == 1 ? bounds : nullptr;
-        FG_LAUNCH(k_sort_count<ITEMS>, dim3(tiles), dim3(kBlock), 0, stream, keys, m, (uint32_t)n_rows, shift, p.bits, p.tiles, counts);
+        FG_LAUNCH((k_sort_count<BLOCK, ITEMS>), dim3(spread), dim3(BLOCK), 0, stream, keys, m, (uint32_t)n_rows, shift, p.bits, p.tiles, counts);
         FG_LAUNCH(k_sort_scan, dim3(1u << p.bits), dim3(kBlock), 0, stream, counts, p.tiles, totals);
-        if (first && last)
-            FG_LAUNCH((k_sort_scatter<ITEMS, true, true>), dim3(spread), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
-                      counts, totals, keys_out, out, place, starts);
-        else if (first)
-            FG_LAUNCH((k_sort_scatter<ITEMS, true, false>), dim3(spread), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
-                      counts, totals, keys_out, out, place, starts);
-        else if (last)
-            FG_LAUNCH((k_sort_scatter<ITEMS, false, true>), dim3(spread), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
-                      counts, totals, keys_out, out, place, starts);
-        else
-            FG_LAUNCH((k_sort_scatter<ITEMS, false, false>), dim3(spread), dim3(kBlock), 0, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,
-                      counts, totals, keys_out, out, place, starts);
+#define FG_SCATTER(FIRST, LAST)                                                                                                          \
+    FG_TRY((scatter<BLOCK, ITEMS, FIRST, LAST>(spread, p.bits, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,          \
+                                               (const uint32_t*)counts, (const uint32_t*)totals, keys_out, out, place, starts)))
+        if (first && last) FG_SCATTER(true, true);
+        else if (first) FG_SCATTER(true, false);
+        else if (last) FG_SCATTER(false, true);
+        else FG_SCATTER(false, false);
+#undef FG_SCATTER
         keys = keys_out;
         from = out;
     }
@@ -379,8 +427,8 @@ hipError_t launch_index_sort(const int32_t* index, int64_t m, int64_t n_rows, in
         if (m <= 2 * kSmallBlock) return small<2>(index, m, n_rows, p, order, place, bounds, workspace, stream);
         return small<8>(index, m, n_rows, p, order, place, bounds, workspace, stream);
     }
-    if (p.items == 4) return many<4>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);
-    return many<16>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);
+    if (!p.large) return many<kBlock, kItems>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);
+    return many<kLargeBlock, kLargeItems>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);
 }
 
 }  // namespace fg

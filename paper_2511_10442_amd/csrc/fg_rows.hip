@@ -15,7 +15,10 @@ namespace {
 
 constexpr int kBlock = 256;
 constexpr int64_t kFill = 256 * 2048;        // lanes that the chip holds at a time
-constexpr int64_t kMostBlocks = 1 << 20;     // more work than that: blocks take several turns
+constexpr int64_t kMostBlocks = 1 << 14;     // eight for every place on the chip; more work than that: blocks take several turns
+constexpr int64_t kMostUneven = 1 << 20;     // the same where pieces differ in what they take: a block that is done makes room for the next
+constexpr int64_t kFewWaves = 256 * 16;      // half of the wavefronts that the chip holds
+constexpr int64_t kStream = 512 << 20;       // bytes that a call moves, twice the last-level cache, from which on most of its output has left that cache
 
 // N elements of a row: 16 bytes, or one element
 template <typename T> constexpr int kWide = 16 / sizeof(T);
@@ -23,12 +26,21 @@ template <typename T, int N>
 struct Piece {
     typedef T Vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
     typedef float Wide __attribute__((ext_vector_type(N)));
-    typedef uint32_t Words __attribute__((ext_vector_type(4)));
+    static constexpr int kWords = N * (int)sizeof(T) / 4;
+    typedef uint32_t Words __attribute__((ext_vector_type(kWords < 1 ? 1 : kWords)));
 };
 template <typename T, int N>
 __device__ __forceinline__ typename Piece<T, N>::Vec load_piece(const T* __restrict__ p) { return *reinterpret_cast<const typename Piece<T, N>::Vec*>(p); }
-template <typename T, int N>
-__device__ __forceinline__ void store_piece(T* __restrict__ p, typename Piece<T, N>::Vec v) { *reinterpret_cast<typename Piece<T, N>::Vec*>(p) = v; }
+// STREAM: past the caches, where nobody would find it there (kStream).  A template argument: of two stores behind a test the compiler makes one
+template <bool STREAM, typename V, typename T>
+__device__ __forceinline__ void store_vec(T* __restrict__ p, V v)
+{
+    typedef V Loose __attribute__((aligned(sizeof(T))));
+    if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<Loose*>(p));
+    else *reinterpret_cast<Loose*>(p) = v;
+}
+template <typename T, int N, bool STREAM = false>
+__device__ __forceinline__ void store_piece(T* __restrict__ p, typename Piece<T, N>::Vec v) { store_vec<STREAM>(p, v); }
 template <typename T, int N>
 __device__ __forceinline__ typename Piece<T, N>::Wide wide(typename Piece<T, N>::Vec v)
 {
@@ -47,107 +59,154 @@ __device__ __forceinline__ typename Piece<T, N>::Vec only_if(bool yes, typename 
     else {
         typename P::Words w = __builtin_bit_cast(typename P::Words, v);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = yes ? w[i] : 0u;
+        for (int i = 0; i < P::kWords; ++i) w[i] = yes ? w[i] : 0u;
         return __builtin_bit_cast(typename P::Vec, w);
     }
 }
 
-// The pieces of all rows in turn.
+// ceil(2^64 / d), for quotients x / d of x < 2^31 d, d <= 2^16 (what M d exceeds 2^64 by, less than d, times x stays below it); d == 1: 0
+struct DivideFar {
+    uint64_t mul;
+    DivideFar() = default;
+    explicit DivideFar(uint32_t d) : mul(d == 1 ? 0 : ~(uint64_t)0 / d + 1) {}
+    __device__ __forceinline__ int64_t operator()(int64_t x) const { return mul == 0 ? x : (int64_t)__umul64hi((uint64_t)x, mul); }
+};
+
+// How the pieces of all rows are dealt out.  One after the other over all lanes: no lane idles whatever a row's width, and every lane works out its
+// row.  Or, where a row's pieces fill wavefronts to three quarters at least, ROWWISE: a wavefront for SEGS x 64 pieces of one row, so that what goes
+// by the row (index, bounds, addresses, branches) is the scalar unit's and a wavefront has several kilobytes under way before it ends.
 struct Deal {
     int64_t total;                           // rows x pieces of a row
-    uint64_t by_pieces_far;                  // ceil(2^64 / pieces): quotients of numbers below 2^31 pieces, for pieces <= 2^16 (FG_MAX_C)
-    uint32_t pieces;
+    int64_t units;                           // rows x wavefronts of a row
+    uint32_t pieces, waves;
     Divide by_pieces;
+    DivideFar by_pieces_far, by_waves_far;
     int32_t c;
-    // the row of piece x; pieces == 1: by_pieces_far would not fit
-    __device__ __forceinline__ int64_t row_of(int64_t x) const { return pieces == 1 ? x : (int64_t)__umul64hi((uint64_t)x, by_pieces_far); }
+    int32_t segs;                            // 0: one after the other
 };
-struct At {
+template <int SEGS>
+struct Span {
     int64_t row;
-    int32_t col;                             // where the piece begins
-    int32_t skip;                            // elements at its beginning that are another's
+    uint32_t piece[SEGS];
+    int32_t col[SEGS];                       // where the piece begins
+    int32_t skip[SEGS];                      // elements at its beginning that are another's
+    bool there[SEGS];                        // (where it isn't, col is the row's last piece)
 };
-template <int N>
-__device__ __forceinline__ At piece_at(const Deal& a, int64_t row0, uint32_t off0, uint32_t ahead)
+template <int N, int SEGS>
+__device__ __forceinline__ Span<SEGS> span_of(const Deal& d, int64_t row, uint32_t piece)
 {
-    const uint32_t x = off0 + ahead, q = a.by_pieces(x);
-    At at;
-    at.row = row0 + q;
-    const int32_t col = (int32_t)(x - q * a.pieces) * N, last = a.c > N ? a.c - N : 0;
-    at.col = col < last ? col : last;
-    at.skip = col - at.col;
+    Span<SEGS> at;
+    at.row = row;
+#pragma unroll
+    for (int s = 0; s < SEGS; ++s) {
+        at.piece[s] = piece + s * 64;
+        const int32_t col = (int32_t)at.piece[s] * N, last = d.c > N ? d.c - N : 0;
+        at.col[s] = col < last ? col : last;
+        at.skip[s] = col - at.col[s];
+        at.there[s] = at.piece[s] < d.pieces;
+    }
     return at;
 }
-
-Deal deal(int64_t rows, int64_t c, uint32_t pieces)
+// SEGS == 0: one after the other
+template <int N, int SEGS, typename Body>
+__device__ __forceinline__ void each_span(const Deal& d, Body&& body)
 {
-    Deal a;
-    a.pieces = pieces;
-    a.total = rows * a.pieces;
-    a.by_pieces = Divide(a.pieces);
-    a.by_pieces_far = a.pieces == 1 ? 0 : ~(uint64_t)0 / a.pieces + 1;      // (2^64 - 1 and 2^64 have the same quotient but where pieces divides 2^64: + 1 is right for both)
-    a.c = (int32_t)c;
-    return a;
+    if constexpr (SEGS > 0) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+        for (int64_t unit = (int64_t)blockIdx.x * (kBlock / 64) + wave; unit < d.units; unit += (int64_t)gridDim.x * (kBlock / 64)) {
+            const int64_t row = d.by_waves_far(unit);
+            body(span_of<N, SEGS>(d, row, (uint32_t)(unit - row * d.waves) * (64 * SEGS) + lane));
+        }
+    } else {
+        for (int64_t first = (int64_t)blockIdx.x * kBlock; first < d.total; first += (int64_t)gridDim.x * kBlock) {
+            const int64_t row0 = d.by_pieces_far(first);
+            const uint32_t x = (uint32_t)(first - row0 * d.pieces) + threadIdx.x, q = d.by_pieces(x);
+            if (first + threadIdx.x < d.total) body(span_of<N, 1>(d, row0 + q, x - q * d.pieces));
+        }
+    }
+}
+
+Deal deal(int64_t rows, int64_t c, uint32_t pieces, int most_segs)
+{
+    Deal d;
+    d.pieces = pieces;
+    d.total = rows * pieces;
+    d.by_pieces = Divide(pieces);
+    d.by_pieces_far = DivideFar(pieces);
+    const uint32_t waves = (pieces + 63) / 64;
+    d.segs = 4 * pieces >= 3 * 64 * waves ? 1 : 0;
+    if (d.segs && most_segs >= 4 && (waves % 4 == 0 || waves >= 12)) d.segs = 4;
+    else if (d.segs && most_segs >= 2 && (waves % 2 == 0 || waves >= 6)) d.segs = 2;
+    // a few rows: a wavefront for each 64 pieces, so that more of the chip has a part
+    if (d.segs && rows * waves < kFewWaves) d.segs = 1;
+    d.waves = d.segs ? (waves + d.segs - 1) / d.segs : 1;
+    d.by_waves_far = DivideFar(d.waves);
+    d.units = rows * d.waves;
+    d.c = (int32_t)c;
+    return d;
 }
 template <typename T, int N>
-Deal deal(int64_t rows, int64_t c) { return deal(rows, c, (uint32_t)((c + N - 1) / N)); }
-unsigned blocks_for(int64_t total, int64_t each)
+Deal deal(int64_t rows, int64_t c, int most_segs) { return deal(rows, c, (uint32_t)((c + N - 1) / N), most_segs); }
+dim3 blocks_for(int64_t total, int64_t each, int64_t most = kMostBlocks)
 {
     const int64_t b = (total + each - 1) / each;
-    return (unsigned)(b < kMostBlocks ? b : kMostBlocks);
+    return dim3((unsigned)(b < most ? b : most));
 }
+dim3 blocks_for(const Deal& d, int64_t most) { return d.segs ? blocks_for(d.units, kBlock / 64, most) : blocks_for(d.total, kBlock, most); }
+// A launch of a kernel by how its pieces are dealt out (SEGS, the kernel's last template argument: up to MOST); N == 1: rows of up to seven elements, one after the other
+#define FG_LAUNCH_DEAL(MOST, d, most, stream, kernel, ...)                                                                                  \
+    do {                                                                                                                              \
+        constexpr int fg_4 = N > 1 && MOST >= 4 ? 4 : 0, fg_2 = N > 1 && MOST >= 2 ? 2 : 0, fg_1 = N > 1 ? 1 : 0;                     \
+        if (fg_4 && (d).segs == 4) FG_LAUNCH((kernel, fg_4>), blocks_for(d, most), dim3(kBlock), 0, stream, __VA_ARGS__);                   \
+        else if (fg_2 && (d).segs == 2) FG_LAUNCH((kernel, fg_2>), blocks_for(d, most), dim3(kBlock), 0, stream, __VA_ARGS__);              \
+        else if (fg_1 && (d).segs == 1) FG_LAUNCH((kernel, fg_1>), blocks_for(d, most), dim3(kBlock), 0, stream, __VA_ARGS__);              \
+        else FG_LAUNCH((kernel, 0>), blocks_for((d).total, kBlock, most), dim3(kBlock), 0, stream, __VA_ARGS__);                            \
+    } while (0)
 
 // ---- lookup ------------------------------------------------------------------------------------------------------------
 
-template <typename T, int N, int AHEAD>
+template <typename T, int N, bool STREAM, int SEGS>
 __global__ __launch_bounds__(kBlock) void k_lookup(const T* __restrict__ table, int64_t table_stride, uint32_t n_rows, const int32_t* __restrict__ index,
                                                    float scale, T* __restrict__ out, int64_t out_stride, Deal d)
 {
     typedef Piece<T, N> P;
-    for (int64_t first = (int64_t)blockIdx.x * (kBlock * AHEAD); first < d.total; first += (int64_t)gridDim.x * (kBlock * AHEAD)) {
-        const int64_t row0 = d.row_of(first);
-        const uint32_t off0 = (uint32_t)(first - row0 * d.pieces);
-        At at[AHEAD];
-        int32_t name[AHEAD];
-        typename P::Vec v[AHEAD];
+    constexpr int S = SEGS ? SEGS : 1;
+    each_span<N, SEGS>(d, [&](const Span<S>& at) {
+        const int32_t name = index[at.row];
+        typename P::Vec v[S] = {};
+        if ((uint32_t)name < n_rows) {
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const uint32_t ahead = u * kBlock + threadIdx.x;
-            at[u] = piece_at<N>(d, row0, off0, ahead);
-            if (first + ahead >= d.total) at[u].row = -1;
-            name[u] = at[u].row < 0 ? -1 : index[at[u].row];
+            for (int s = 0; s < S; ++s) v[s] = load_piece<T, N>(table + (int64_t)name * table_stride + at.col[s]);
+#pragma unroll
+            for (int s = 0; s < S; ++s) v[s] = narrow<T, N>(wide<T, N>(v[s]) * scale);
         }
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            v[u] = typename P::Vec{};
-            if ((uint32_t)name[u] < n_rows) v[u] = load_piece<T, N>(table + (int64_t)name[u] * table_stride + at[u].col);
-        }
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-            if (at[u].row >= 0) {
-                typename P::Wide x = wide<T, N>(v[u]) * scale;
-                if ((uint32_t)name[u] >= n_rows) x = typename P::Wide{};           // also where the scale is not finite
-                store_piece<T, N>(out + at[u].row * out_stride + at[u].col, narrow<T, N>(x));
-            }
-    }
+        for (int s = 0; s < S; ++s)
+            if (at.there[s]) store_piece<T, N, STREAM>(out + at.row * out_stride + at.col[s], v[s]);
+    });
 }
 
 // ---- a token's row to its places ---------------------------------------------------------------------------------------
 
-template <typename T, int N>
+template <typename T, int N, int SEGS>
 __global__ __launch_bounds__(kBlock) void k_dispatch(const T* __restrict__ x, int64_t x_stride, const int32_t* __restrict__ place, int32_t k,
                                                      uint32_t n_rows, T* __restrict__ out, int64_t out_stride, Deal d)
 {
     typedef Piece<T, N> P;
-    for (int64_t first = (int64_t)blockIdx.x * kBlock; first < d.total; first += (int64_t)gridDim.x * kBlock) {
-        const int64_t row0 = d.row_of(first);
-        const At at = piece_at<N>(d, row0, (uint32_t)(first - row0 * d.pieces), threadIdx.x);
-        if (first + threadIdx.x >= d.total) continue;
-        const typename P::Vec v = load_piece<T, N>(x + at.row * x_stride + at.col);
+    constexpr int S = SEGS ? SEGS : 1;
+    each_span<N, SEGS>(d, [&](const Span<S>& at) {
+        typename P::Vec v[S];
+#pragma unroll
+        for (int s = 0; s < S; ++s) v[s] = load_piece<T, N>(x + at.row * x_stride + at.col[s]);
         const int32_t* p = place + at.row * k;
-        for (int32_t j = 0; j < k; ++j)
-            if ((uint32_t)p[j] < n_rows) store_piece<T, N>(out + (int64_t)p[j] * out_stride + at.col, v);
-    }
+        for (int32_t j = 0; j < k; ++j) {
+            const int32_t to = p[j];
+            if ((uint32_t)to < n_rows)
+#pragma unroll
+                for (int s = 0; s < S; ++s)
+                    if (at.there[s]) store_piece<T, N>(out + (int64_t)to * out_stride + at.col[s], v[s]);
+        }
+    });
 }
 
 // ---- entries, several at a time ----------------------------------------------------------------------------------------
@@ -167,56 +226,59 @@ __device__ __forceinline__ void load_words(const W* __restrict__ p, int there, W
     }
 }
 
-// Calls body(U, first, there) over [0, n): eight at a time, the last of a list in one go as 8, 4 or 1 of which `there` are there, so that a short list
-// costs one trip to memory and few loads that nobody asked for.
-template <int N> struct Count { static constexpr int value = N; };
-template <typename Body>
+// Calls body(U, first, there) over [0, n): MOST (8, 4 or 2) at a time, the last of a list in one go as MOST, half of it or 1 of which `there` are
+// there, so that a short list costs one trip to memory and few loads that nobody asked for.
+template <int U> struct Count { static constexpr int value = U; };
+template <int MOST, typename Body>
 __device__ __forceinline__ void in_chunks(int32_t n, Body&& body)
 {
     int32_t at = 0;
 #pragma unroll 1
-    for (; n - at > 4; at += 8) body(Count<8>{}, at, n - at < 8 ? n - at : 8);
-    if (n - at > 1) body(Count<4>{}, at, n - at);
+    for (; n - at > MOST / 2; at += MOST) body(Count<MOST>{}, at, n - at < MOST ? n - at : MOST);
+    if (MOST > 2 && n - at > 1) body(Count<MOST / 2>{}, at, n - at);
     else if (n - at == 1) body(Count<1>{}, at, 1);
 }
 
 // ---- weighted sums -----------------------------------------------------------------------------------------------------
 
 // (n_rows > 0: an entry that names no row reads row 0 and adds zeros in its place, so that no load waits behind a branch)
-template <typename T, int N, bool WEIGHTED>
+template <typename T, int N, bool WEIGHTED, bool STREAM, int SEGS>
 __global__ __launch_bounds__(kBlock) void k_combine(const T* __restrict__ rows, int64_t rows_stride, uint32_t n_rows, const int32_t* __restrict__ index,
                                                     const float* __restrict__ weights, int32_t k, T* __restrict__ out, int64_t out_stride, Deal d)
 {
     typedef Piece<T, N> P;
-    for (int64_t first = (int64_t)blockIdx.x * kBlock; first < d.total; first += (int64_t)gridDim.x * kBlock) {
-        const int64_t row0 = d.row_of(first);
-        const At at = piece_at<N>(d, row0, (uint32_t)(first - row0 * d.pieces), threadIdx.x);
-        if (first + threadIdx.x >= d.total) continue;
-        typename P::Wide sum = {};
+    constexpr int S = SEGS ? SEGS : 1;
+    each_span<N, SEGS>(d, [&](const Span<S>& at) {
+        typename P::Wide sum[S] = {};
         const int64_t base = at.row * k;
-        in_chunks(k, [&](auto count, int32_t j, int there) {
+        in_chunks<8>(k, [&](auto count, int32_t j, int there) {
             constexpr int U = count.value;
             int32_t name[U];
             float w[U];
-            typename P::Vec v[U];
+            typename P::Vec v[U][S];
             load_words<U>(index + base + j, there, name);
             if (WEIGHTED) load_words<U>(weights + base + j, there, w);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const bool named = u < there && (uint32_t)name[u] < n_rows;
-                v[u] = load_piece<T, N>(rows + (named ? (int64_t)name[u] : 0) * rows_stride + at.col);
+#pragma unroll
+                for (int s = 0; s < S; ++s) v[u][s] = load_piece<T, N>(rows + (named ? (int64_t)name[u] : 0) * rows_stride + at.col[s]);
                 if (WEIGHTED) w[u] = named ? w[u] : 0.0f;
                 name[u] = named;
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const typename P::Wide x = wide<T, N>(only_if<T, N>(name[u], v[u]));
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int i = 0; i < N; ++i) sum[i] = WEIGHTED ? __builtin_fmaf(x[i], w[u], sum[i]) : sum[i] + x[i];
-            }
+                for (int s = 0; s < S; ++s) {
+                    const typename P::Wide x = wide<T, N>(only_if<T, N>(name[u], v[u][s]));
+#pragma unroll
+                    for (int i = 0; i < N; ++i) sum[s][i] = WEIGHTED ? __builtin_fmaf(x[i], w[u], sum[s][i]) : sum[s][i] + x[i];
+                }
         });
-        store_piece<T, N>(out + at.row * out_stride + at.col, narrow<T, N>(sum));
-    }
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+            if (at.there[s]) store_piece<T, N, STREAM>(out + at.row * out_stride + at.col[s], narrow<T, N>(sum[s]));
+    });
 }
 
 // ---- gradients of weights, and of rows that are named once -------------------------------------------------------------
@@ -242,7 +304,7 @@ __device__ __forceinline__ float add_eight(float (&x)[8], int lane, int lanes)
     return sum;
 }
 
-// `lanes` lanes (a power of two from 8 to 64, or 128 or 256: WAVES of them, which meet in LDS) take a token: they walk along its row and those of up
+// `lanes` lanes (8 to 32: WAVES == 0; 64, 128 or 256: WAVES wavefronts, which meet in LDS) take a token: they walk along its row and those of up
 // to eight of its k, so that the token's gradient is loaded once for the eight.
 template <typename T, int N, bool ROWS, bool WEIGHTED, int WAVES>
 __global__ __launch_bounds__(kBlock, ROWS ? 3 : 4) void k_combine_grad(const T* __restrict__ grad_out, int64_t grad_stride, int64_t t, int32_t c,
@@ -258,7 +320,8 @@ __global__ __launch_bounds__(kBlock, ROWS ? 3 : 4) void k_combine_grad(const T* 
     const int64_t turns = (t + each - 1) / each;
     const bool dots = grad_weights && n_rows > 0;
     for (int64_t turn = blockIdx.x; turn < turns; turn += gridDim.x) {
-        const int64_t row = turn * each + (threadIdx.x >> log);
+        const int group = WAVES ? __builtin_amdgcn_readfirstlane(threadIdx.x >> log) : threadIdx.x >> log;
+        const int64_t row = turn * each + group;
         const bool there = row < t;
         const int64_t base = there ? row * k : 0;
         for (int32_t j0 = 0; j0 < k; j0 += 8) {
@@ -302,7 +365,7 @@ __global__ __launch_bounds__(kBlock, ROWS ? 3 : 4) void k_combine_grad(const T* 
             // (products with row 0, of entries that name none, are dropped here, NaN and all)
 #pragma unroll
             for (int u = 0; u < 8; ++u) dot[u] = name[u] < 0 ? 0.0f : dot[u];
-            const int some = WAVES > 1 ? 64 : lanes;
+            const int some = WAVES ? 64 : lanes;
             float sum = add_eight(dot, threadIdx.x & (some - 1), some);
             const int u = eighth(threadIdx.x & (some - 1), some);
             bool writes = (threadIdx.x & (some / 8 - 1)) == 0;
@@ -324,10 +387,14 @@ __global__ __launch_bounds__(kBlock, ROWS ? 3 : 4) void k_combine_grad(const T* 
 // ---- sums over the entries of a row ------------------------------------------------------------------------------------
 
 // Rows that are named often are summed in parts: `chunk` entries of the sorted index that all name one row, and kChunks such chunks, are summed
-// beforehand, so that what one lane does for a row hardly grows with the row's entries.  chunk is kChunk, or where there are rows enough to
-// fill the chip, four times the mean of a row's entries (a power of two): rows of a graph are named often, but all of them.
+// by themselves and put together afterwards, so that what one lane does for a row hardly grows with the row's entries.  chunk is kChunk, or where
+// there are rows enough to fill the chip, four times the mean of a row's entries (a power of two): rows of a graph are named often, but all of them.
+//   k_row_sums   chunks of one row each: their sums; rows without such a chunk: from their entries
+//   k_row_parts  chunks of chunks (where there are enough entries)
+//   k_row_join   rows with a chunk: the entries before it, chunks up to the first whole chunk of chunks, those, and so back
+// The long rows' entries are read while the many short ones are written.
 constexpr int kChunk = 32, kChunks = 32;
-constexpr int64_t kParts2From = 16;          // chunks of chunks from which on it is looked whether there are any
+constexpr int64_t kPartsFrom = 16;           // chunks of chunks from which on it is looked whether there are any
 
 struct SumArgs {
     const int32_t *index, *order, *bounds;
@@ -335,7 +402,7 @@ struct SumArgs {
     float* grad_weights;     // DOTS
     int32_t m;
     int64_t n_rows;
-    int32_t fan;
+    int64_t chunks;          // m / chunk
     Divide by_fan;
     float scale;
     int32_t shift;           // log2 of chunk
@@ -344,16 +411,16 @@ struct SumArgs {
 
 // Adds the entries [from, to) of the sorted index to sum.  DOTS: their products with `row` (the piece of the row that they name) are added up over
 // the `lanes` lanes that share it and written as their weights' gradients; `real`: this lane has a piece.
-template <typename T, int N, bool WEIGHTED, bool DOTS>
-__device__ __forceinline__ void add_entries(typename Piece<T, N>::Wide& sum, const SumArgs& a, const T* __restrict__ grad, int64_t grad_stride, int32_t from,
-                                            int32_t to, int32_t col, int32_t c, const typename Piece<T, N>::Wide& row, bool real, int lanes)
+template <typename T, int N, bool WEIGHTED, bool DOTS, int S>
+__device__ __forceinline__ void add_entries(typename Piece<T, N>::Wide (&sum)[S], const SumArgs& a, const T* __restrict__ grad, int64_t grad_stride,
+                                            int32_t from, int32_t to, const Span<S>& at, const typename Piece<T, N>::Wide& row, bool real, int lanes)
 {
     typedef Piece<T, N> P;
-    in_chunks(to - from, [&](auto count, int32_t p, int there) {
+    in_chunks<(16 / S < 8 ? 16 / S : 8)>(to - from, [&](auto count, int32_t p, int there) {
         constexpr int U = count.value;
         int32_t entry[U];
         float w[U];
-        typename P::Vec v[U];
+        typename P::Vec v[U][S];
         load_words<U>(a.order + from + p, there, entry);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -361,20 +428,22 @@ __device__ __forceinline__ void add_entries(typename Piece<T, N>::Wide& sum, con
             w[u] = WEIGHTED ? a.weights[entry[u]] : 1.0f;
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            // (fan == 1: the division by one)
-            v[u] = load_piece<T, N>(grad + (int64_t)a.by_fan((uint32_t)entry[u]) * grad_stride + col);
-        }
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int s = 0; s < S; ++s) v[u][s] = load_piece<T, N>(grad + (int64_t)a.by_fan((uint32_t)entry[u]) * grad_stride + at.col[s]);
         float dot[8];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const typename P::Wide x = wide<T, N>(only_if<T, N>(u < there && (!DOTS || real), v[u]));
             if (WEIGHTED) w[u] = u < there ? w[u] : 0.0f;
             float products = 0.0f;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                sum[i] = WEIGHTED ? __builtin_fmaf(x[i], w[u], sum[i]) : sum[i] + x[i];
-                if (DOTS) products = __builtin_fmaf(x[i], row[i], products);
+            for (int s = 0; s < S; ++s) {
+                const typename P::Wide x = wide<T, N>(only_if<T, N>(u < there && (!DOTS || real), v[u][s]));
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    sum[s][i] = WEIGHTED ? __builtin_fmaf(x[i], w[u], sum[s][i]) : sum[s][i] + x[i];
+                    if (DOTS) products = __builtin_fmaf(x[i], row[i], products);
+                }
             }
             dot[u] = products;
         }
@@ -391,11 +460,12 @@ __device__ __forceinline__ void add_entries(typename Piece<T, N>::Wide& sum, con
     });
 }
 
+// Adds the sums [from, to) of `parts`, one after the other every `stride`.
 template <typename T, int N>
 __device__ __forceinline__ void add_parts(typename Piece<T, N>::Wide& sum, const float* __restrict__ parts, int64_t stride, int32_t from, int32_t to)
 {
     typedef typename Piece<T, N>::Wide Wide;
-    constexpr int U = 4;
+    constexpr int U = N > 4 ? 4 : 8;
 #pragma unroll 1
     for (int32_t q = from; q < to; q += U) {
         Wide v[U];
@@ -416,127 +486,122 @@ __device__ __forceinline__ bool one_row(const SumArgs& a, int32_t p, int32_t n, 
     return name == a.index[e1] && (uint32_t)name < (uint32_t)a.n_rows;
 }
 
-template <typename T, int N, bool WEIGHTED, bool DOTS>
-__global__ __launch_bounds__(kBlock) void k_row_parts(SumArgs a, const T* __restrict__ grad, int64_t grad_stride, const T* __restrict__ rows,
-                                                      int64_t rows_stride, Deal d)
+__device__ __forceinline__ void range_of(const SumArgs& a, int64_t row, int32_t& from, int32_t& to)
 {
-    typedef Piece<T, N> P;
-    for (int64_t first = (int64_t)blockIdx.x * kBlock; first < d.total; first += (int64_t)gridDim.x * kBlock) {
-        const int64_t row0 = d.row_of(first);
-        const uint32_t off0 = (uint32_t)(first - row0 * d.pieces);
-        const At at = piece_at<N>(d, row0, off0, threadIdx.x);
-        if (first + threadIdx.x >= d.total) continue;
-        const int32_t p = (int32_t)at.row << a.shift, n = 1 << a.shift;
-        int32_t name;
-        if (!one_row(a, p, n, name)) continue;
-        float* part = a.parts + (first + threadIdx.x) * N;             // piece after piece: no piece of these overlaps another
-        const bool real = at.skip < N;
-        if constexpr (DOTS) {
-            const typename P::Wide row = wide<T, N>(load_piece<T, N>(rows + (int64_t)name * rows_stride + at.col));
-            typename P::Wide sum = {};
-            add_entries<T, N, WEIGHTED, true>(sum, a, grad, grad_stride, p, p + n, at.col, d.c, row, real, (int)d.pieces);
-            if (real) *reinterpret_cast<typename P::Wide*>(part) = sum;
+    from = a.bounds[row];
+    to = a.bounds[row + 1];
+    from = from < 0 ? 0 : from;
+    to = to > a.m ? a.m : to;
+}
+__device__ __forceinline__ int32_t first_chunk(const SumArgs& a, int32_t from) { return (int32_t)(((int64_t)from + (1 << a.shift) - 1) >> a.shift); }
+
+template <typename T, int N, typename TO, bool ACCUMULATE, bool STREAM, int S>
+__device__ __forceinline__ void store_sum(const SumArgs& a, typename Piece<T, N>::Wide (&sum)[S], TO* __restrict__ out, int64_t out_stride, int64_t row,
+                                          const Span<S>& at)
+{
+    typedef TO OutVec __attribute__((ext_vector_type(N), aligned(sizeof(TO))));
+    typedef typename Piece<T, N>::Wide Wide;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        if (!at.there[s] || at.skip[s] >= N) continue;
+        TO* p = out + row * out_stride + at.col[s];
+        Wide x = sum[s] * a.scale;
+        if (!ACCUMULATE || at.skip[s] == 0) {
+            if (ACCUMULATE) x += __builtin_convertvector(*reinterpret_cast<const OutVec*>(p), Wide);
+            store_vec<STREAM>(p, __builtin_convertvector(x, OutVec));
         } else {
-            typename P::Wide sum = {};
-            add_entries<T, N, WEIGHTED, false>(sum, a, grad, grad_stride, p, p + n, at.col, d.c, sum, true, 0);
-            *reinterpret_cast<typename P::Wide*>(part) = sum;
+            // (added once: elements that the piece before covers are left to it)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i >= at.skip[s]) p[i] = (TO)(x[i] + (float)p[i]);
         }
     }
+}
+
+template <typename T, int N, typename TO, bool WEIGHTED, bool ACCUMULATE, bool DOTS, bool STREAM, int SEGS>
+__global__ __launch_bounds__(kBlock, DOTS && sizeof(T) == 2 ? 3 : 4) void k_row_sums(SumArgs a, const int32_t* __restrict__ index, const int32_t* __restrict__ order,
+                                                                                     const int32_t* __restrict__ bounds, const float* __restrict__ weights,
+                                                                                     const T* __restrict__ grad, int64_t grad_stride,
+                                                                                     const T* __restrict__ rows, int64_t rows_stride,
+                                                                                     TO* __restrict__ out, int64_t out_stride, Deal d)
+{
+    typedef Piece<T, N> P;
+    constexpr int S = SEGS ? SEGS : 1;
+    a.index = index; a.order = order; a.bounds = bounds; a.weights = weights;        // (arguments of their own: nothing stored changes them)
+    each_span<N, SEGS>(d, [&](const Span<S>& at) {
+        const bool real = !DOTS || at.skip[0] < N;
+        const bool is_chunk = at.row < a.chunks;
+        int64_t name = at.row - a.chunks;
+        int32_t from, to;
+        if (is_chunk) {
+            int32_t of;
+            from = (int32_t)at.row << a.shift;
+            to = from + (1 << a.shift);
+            if (!one_row(a, from, 1 << a.shift, of)) return;
+            name = of;
+        } else {
+            range_of(a, name, from, to);
+            if (first_chunk(a, from) < to >> a.shift) return;              // k_row_join
+            if (ACCUMULATE && from >= to) return;
+        }
+        typename P::Wide sum[S] = {}, row = {};
+        if (DOTS && from < to) row = wide<T, N>(load_piece<T, N>(rows + name * rows_stride + at.col[0]));
+        add_entries<T, N, WEIGHTED, DOTS, S>(sum, a, grad, grad_stride, from, to, at, row, real, (int)d.pieces);
+        if (is_chunk) {
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+                if (real && at.there[s]) *reinterpret_cast<typename P::Wide*>(a.parts + (at.row * d.pieces + at.piece[s]) * N) = sum[s];
+        } else {
+            store_sum<T, N, TO, ACCUMULATE, STREAM, S>(a, sum, out, out_stride, name, at);
+        }
+    });
 }
 
 template <typename T, int N>
-__global__ __launch_bounds__(kBlock) void k_row_parts_of_parts(SumArgs a, Deal d)
+__global__ __launch_bounds__(kBlock) void k_row_parts(SumArgs a, Deal d)
 {
-    typedef Piece<T, N> P;
-    for (int64_t first = (int64_t)blockIdx.x * kBlock; first < d.total; first += (int64_t)gridDim.x * kBlock) {
-        const int64_t row0 = d.row_of(first);
-        const uint32_t x = (uint32_t)(first - row0 * d.pieces) + threadIdx.x, q = d.by_pieces(x);
-        if (first + threadIdx.x >= d.total) continue;
-        const int64_t r = row0 + q;
+    each_span<N, 0>(d, [&](const Span<1>& at) {
         int32_t name;
-        if (!one_row(a, (int32_t)(r * kChunks) << a.shift, kChunks << a.shift, name)) continue;
-        const int64_t stride = (int64_t)d.pieces * N;
-        typename P::Wide sum = {};
-        add_parts<T, N>(sum, a.parts + (x - q * d.pieces) * N, stride, (int32_t)r * kChunks, (int32_t)(r + 1) * kChunks);
-        *reinterpret_cast<typename P::Wide*>(a.parts2 + (first + threadIdx.x) * N) = sum;
-    }
+        if (!one_row(a, (int32_t)(at.row * kChunks) << a.shift, kChunks << a.shift, name)) return;
+        typename Piece<T, N>::Wide sum = {};
+        add_parts<T, N>(sum, a.parts + at.piece[0] * N, (int64_t)d.pieces * N, (int32_t)at.row * kChunks, (int32_t)(at.row + 1) * kChunks);
+        *reinterpret_cast<typename Piece<T, N>::Wide*>(a.parts2 + (at.row * d.pieces + at.piece[0]) * N) = sum;
+    });
 }
 
-// A row's entries: single ones up to the first whole chunk, chunks up to the first whole chunk of chunks, and so back.  `piece`: of the row.
-template <typename T, int N, bool WEIGHTED, bool DOTS>
-__device__ __forceinline__ void add_row(typename Piece<T, N>::Wide& sum, const SumArgs& a, const T* __restrict__ grad, int64_t grad_stride, int32_t from,
-                                        int32_t to, int32_t col, int32_t c, uint32_t piece, uint32_t pieces, const typename Piece<T, N>::Wide& row, bool real)
-{
-    const int32_t q0 = (from + (1 << a.shift) - 1) >> a.shift, q1 = to >> a.shift;
-    const bool parts = q0 < q1;
-    // (the single entries before and after the chunks in one loop's code)
-#pragma unroll 1
-    for (int side = 0; side < 2; ++side) {
-        add_entries<T, N, WEIGHTED, DOTS>(sum, a, grad, grad_stride, side ? q1 << a.shift : from, side || !parts ? to : q0 << a.shift, col, c, row, real,
-                                             (int)pieces);
-        if (side || !parts) return;
-        const int64_t stride = (int64_t)pieces * N;
-        const float *at = a.parts + piece * N, *at2 = a.parts2 + piece * N;
-        const int32_t r0 = a.parts2 ? (q0 + kChunks - 1) / kChunks : q1, r1 = a.parts2 ? q1 / kChunks : 0;
-        if (r0 < r1) {
-            add_parts<T, N>(sum, at, stride, q0, r0 * kChunks);
-            add_parts<T, N>(sum, at2, stride, r0, r1);
-            add_parts<T, N>(sum, at, stride, r1 * kChunks, q1);
-        } else {
-            add_parts<T, N>(sum, at, stride, q0, q1);
-        }
-    }
-}
-
-// Most rows of a large table have no entry and a store of zeros is all their work; a block takes `turns` runs of pieces and asks for the next run's
-// bounds before it works on one.
-constexpr int kTurns = 4;
 template <typename T, int N, typename TO, bool WEIGHTED, bool ACCUMULATE, bool DOTS>
-__global__ __launch_bounds__(kBlock, DOTS && sizeof(T) == 2 ? 3 : 4) void k_row_sums(SumArgs a, const T* __restrict__ grad, int64_t grad_stride, const T* __restrict__ rows,
-                                                     int64_t rows_stride, TO* __restrict__ out, int64_t out_stride, Deal d, int turns)
+__global__ __launch_bounds__(kBlock) void k_row_join(SumArgs a, const T* __restrict__ grad, int64_t grad_stride, const T* __restrict__ rows,
+                                                     int64_t rows_stride, TO* __restrict__ out, int64_t out_stride, Deal d)
 {
     typedef Piece<T, N> P;
-    typedef TO OutVec __attribute__((ext_vector_type(N), aligned(sizeof(TO))));
-    for (int64_t first = (int64_t)blockIdx.x * (kBlock * turns); first < d.total; first += (int64_t)gridDim.x * (kBlock * turns)) {
-        const int64_t row0 = d.row_of(first);
-        const uint32_t off0 = (uint32_t)(first - row0 * d.pieces);
-        At next = piece_at<N>(d, row0, off0, threadIdx.x);
-        int32_t from_next = 0, to_next = 0;
-        if (first + threadIdx.x < d.total) { from_next = a.bounds[next.row]; to_next = a.bounds[next.row + 1]; }
-        for (int turn = 0; turn < turns; ++turn) {
-            const uint32_t ahead = (uint32_t)turn * kBlock + threadIdx.x;
-            if (first + ahead >= d.total) break;
-            const At at = next;
-            int32_t from = from_next, to = to_next;
-            if (turn + 1 < turns && first + ahead + kBlock < d.total) {
-                next = piece_at<N>(d, row0, off0, ahead + kBlock);
-                from_next = a.bounds[next.row];
-                to_next = a.bounds[next.row + 1];
-            }
-            from = from < 0 ? 0 : from;
-            to = to > a.m ? a.m : to;
-            if (ACCUMULATE && from >= to) continue;
-            const uint32_t piece = (uint32_t)(at.col + at.skip) / N;
-            const bool real = at.skip < N;
-            TO* p = out + at.row * out_stride + at.col;
-            typename P::Wide sum = {}, row = {};
-            if (from < to) {
-                if (DOTS) row = wide<T, N>(load_piece<T, N>(rows + at.row * rows_stride + at.col));
-                add_row<T, N, WEIGHTED, DOTS>(sum, a, grad, grad_stride, from, to, at.col, d.c, piece, d.pieces, row, real);
-            }
-            sum *= a.scale;
-            if (!ACCUMULATE || at.skip == 0) {
-                OutVec* q = reinterpret_cast<OutVec*>(p);
-                if (ACCUMULATE) sum += __builtin_convertvector(*q, typename P::Wide);
-                if (!DOTS || real) *q = __builtin_convertvector(sum, OutVec);
+    each_span<N, 0>(d, [&](const Span<1>& at) {
+        int32_t name, from, to;
+        const int32_t q0 = (int32_t)at.row;
+        if (!one_row(a, q0 << a.shift, 1 << a.shift, name)) return;
+        range_of(a, name, from, to);
+        const int32_t q1 = to >> a.shift;
+        if (first_chunk(a, from) != q0 || q0 >= q1) return;                // the row's first chunk has the row
+        const bool real = !DOTS || at.skip[0] < N;
+        typename P::Wide sum[1] = {}, row = {};
+        if (DOTS) row = wide<T, N>(load_piece<T, N>(rows + (int64_t)name * rows_stride + at.col[0]));
+        const int64_t stride = (int64_t)d.pieces * N;
+        const float *parts = a.parts + at.piece[0] * N, *parts2 = a.parts2 + at.piece[0] * N;
+        const int32_t r0 = a.parts2 ? (q0 + kChunks - 1) / kChunks : q1, r1 = a.parts2 ? q1 / kChunks : 0;
+        // (the single entries before and after the chunks in one loop's code)
+#pragma unroll 1
+        for (int side = 0; side < 2; ++side) {
+            add_entries<T, N, WEIGHTED, DOTS, 1>(sum, a, grad, grad_stride, side ? q1 << a.shift : from, side ? to : q0 << a.shift, at, row, real, (int)d.pieces);
+            if (side) break;
+            if (r0 < r1) {
+                add_parts<T, N>(sum[0], parts, stride, q0, r0 * kChunks);
+                add_parts<T, N>(sum[0], parts2, stride, r0, r1);
+                add_parts<T, N>(sum[0], parts, stride, r1 * kChunks, q1);
             } else {
-                // (added once: elements that the piece before covers are left to it)
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (i >= at.skip) p[i] = (TO)(sum[i] + (float)p[i]);
+                add_parts<T, N>(sum[0], parts, stride, q0, q1);
             }
         }
-    }
+        store_sum<T, N, TO, ACCUMULATE, false, 1>(a, sum, out, out_stride, name, at);
+    });
 }
 
 // Weights' gradients of entries that name no row.
@@ -566,28 +631,35 @@ hipError_t row_sums(const RowSums& r, const SumArgs& a, hipStream_t stream)
     // with products a row's lanes are a power of two, so that they lie in one wavefront
     uint32_t pieces = (uint32_t)((r.c + N - 1) / N);
     if (DOTS) pieces = lanes_for(pieces);
-    const Deal d = deal(r.n_rows, r.c, pieces);
     SumArgs b = a;
     int64_t chunk = kChunk;
     b.shift = 5;
-    while (d.total >= kFill && chunk < 4 * (r.m / r.n_rows) && chunk < 65536) { chunk *= 2; ++b.shift; }
+    while (r.n_rows * pieces >= kFill && chunk < 4 * (r.m / r.n_rows) && chunk < 65536) { chunk *= 2; ++b.shift; }
+    b.chunks = r.m / chunk;
     b.parts = r.partials;
     b.parts2 = nullptr;
-    const int64_t chunks = r.m / chunk, chunks2 = chunks / kChunks;
-    if (chunks) {
-        const Deal dp = deal(chunks, r.c, pieces);
-        FG_LAUNCH((k_row_parts<T, N, WEIGHTED, DOTS>), dim3(blocks_for(dp.total, kBlock)), dim3(kBlock), 0, stream, b, grad, r.grad.stride, rows,
-                  r.rows.stride, dp);
+    const Deal d = deal(b.chunks + r.n_rows, r.c, pieces, DOTS ? 1 : 4);
+#define FG_SUMS(STREAM) k_row_sums<T, N, TO, WEIGHTED, ACCUMULATE, DOTS, STREAM
+#define FG_SUMS_ARGS b, b.index, b.order, b.bounds, b.weights, grad, r.grad.stride, rows, r.rows.stride, (TO*)r.out.at, r.out.stride, d
+    if constexpr (DOTS) {
+        FG_LAUNCH_DEAL(1, d, kMostUneven, stream, FG_SUMS(false), FG_SUMS_ARGS);
+        FG_LAUNCH(k_no_rows, blocks_for((r.m + 15) / 16, kBlock), dim3(kBlock), 0, stream, b);
+    } else if (ACCUMULATE || (r.n_rows * (int64_t)sizeof(TO) + r.m / r.fan * (int64_t)sizeof(T)) * r.c < kStream) {
+        FG_LAUNCH_DEAL(4, d, kMostUneven, stream, FG_SUMS(false), FG_SUMS_ARGS);
+    } else {
+        FG_LAUNCH_DEAL(4, d, kMostUneven, stream, FG_SUMS(!ACCUMULATE), FG_SUMS_ARGS);
     }
-    if (chunks2 >= kParts2From) {
-        b.parts2 = r.partials + chunks * ((int64_t)pieces * N);
-        const Deal dp = deal(chunks2, r.c, pieces);
-        FG_LAUNCH((k_row_parts_of_parts<T, N>), dim3(blocks_for(dp.total, kBlock)), dim3(kBlock), 0, stream, b, dp);
+#undef FG_SUMS_ARGS
+#undef FG_SUMS
+    if (!b.chunks) return hipSuccess;
+    if (b.chunks / kChunks >= kPartsFrom) {
+        b.parts2 = r.partials + b.chunks * ((int64_t)pieces * N);
+        const Deal dp = deal(b.chunks / kChunks, r.c, pieces, 0);
+        FG_LAUNCH((k_row_parts<T, N>), blocks_for(dp.total, kBlock), dim3(kBlock), 0, stream, b, dp);
     }
-    const int turns = d.total >= (int64_t)kBlock * kTurns * 2048 ? kTurns : 1;
-    FG_LAUNCH((k_row_sums<T, N, TO, WEIGHTED, ACCUMULATE, DOTS>), dim3(blocks_for(d.total, kBlock * turns)), dim3(kBlock), 0, stream, b, grad,
-              r.grad.stride, rows, r.rows.stride, (TO*)r.out.at, r.out.stride, d, turns);
-    if (DOTS) FG_LAUNCH(k_no_rows, dim3(blocks_for((r.m + 15) / 16, kBlock)), dim3(kBlock), 0, stream, b);
+    const Deal dj = deal(b.chunks, r.c, pieces, 0);
+    FG_LAUNCH((k_row_join<T, N, TO, WEIGHTED, ACCUMULATE, DOTS>), blocks_for(dj.total, kBlock), dim3(kBlock), 0, stream, b, grad, r.grad.stride, rows,
+              r.rows.stride, (TO*)r.out.at, r.out.stride, dj);
     return hipSuccess;
 }
 
@@ -605,23 +677,23 @@ hipError_t row_sums_of(const RowSums& r, const SumArgs& a, hipStream_t stream)
 template <typename T, int N>
 hipError_t lookup(RowsIn table, int64_t n_rows, int64_t c, const int32_t* index, int64_t m, float scale, RowsOut out, hipStream_t stream)
 {
-    constexpr int kFour = 4;
-    const Deal d = deal<T, N>(m, c);
-    if (d.total < 1024 * kBlock * kFour)
-        FG_LAUNCH((k_lookup<T, N, 1>), dim3(blocks_for(d.total, kBlock)), dim3(kBlock), 0, stream, (const T*)table.at, table.stride, (uint32_t)n_rows, index,
-                  scale, (T*)out.at, out.stride, d);
-    else
-        FG_LAUNCH((k_lookup<T, N, kFour>), dim3(blocks_for(d.total, kBlock * kFour)), dim3(kBlock), 0, stream, (const T*)table.at, table.stride,
-                  (uint32_t)n_rows, index, scale, (T*)out.at, out.stride, d);
+    const Deal d = deal<T, N>(m, c, 2);
+#define FG_LOOKUP(STREAM) \
+    FG_LAUNCH_DEAL(2, d, kMostBlocks, stream, FG_LOOKUP_OF(STREAM), (const T*)table.at, table.stride, (uint32_t)n_rows, index, scale, (T*)out.at, out.stride, d)
+#define FG_LOOKUP_OF(STREAM) k_lookup<T, N, STREAM
+    if (2 * m * c * (int64_t)sizeof(T) < kStream) FG_LOOKUP(false); else FG_LOOKUP(true);
+#undef FG_LOOKUP_OF
+#undef FG_LOOKUP
     return hipSuccess;
 }
 
 template <typename T, int N>
 hipError_t dispatch(RowsIn x, int64_t t, int64_t c, const int32_t* place, int32_t k, int64_t n_rows, RowsOut out, hipStream_t stream)
 {
-    const Deal d = deal<T, N>(t, c);
-    FG_LAUNCH((k_dispatch<T, N>), dim3(blocks_for(d.total, kBlock)), dim3(kBlock), 0, stream, (const T*)x.at, x.stride, place, k, (uint32_t)n_rows, (T*)out.at,
-              out.stride, d);
+    const Deal d = deal<T, N>(t, c, 4);
+#define FG_DISPATCH k_dispatch<T, N
+    FG_LAUNCH_DEAL(4, d, kMostBlocks, stream, FG_DISPATCH, (const T*)x.at, x.stride, place, k, (uint32_t)n_rows, (T*)out.at, out.stride, d);
+#undef FG_DISPATCH
     return hipSuccess;
 }
 
@@ -630,14 +702,16 @@ hipError_t combine(RowsIn rows, int64_t n_rows, int64_t c, const int32_t* index,
                    hipStream_t stream)
 {
     if (n_rows == 0) return lookup<T, N>(rows, 0, c, index, t, 1.0f, out, stream);       // zeros
-    const Deal d = deal<T, N>(t, c);
-    const dim3 grid(blocks_for(d.total, kBlock));
-    if (weights)
-        FG_LAUNCH((k_combine<T, N, true>), grid, dim3(kBlock), 0, stream, (const T*)rows.at, rows.stride, (uint32_t)n_rows, index, weights, k, (T*)out.at,
-                  out.stride, d);
-    else
-        FG_LAUNCH((k_combine<T, N, false>), grid, dim3(kBlock), 0, stream, (const T*)rows.at, rows.stride, (uint32_t)n_rows, index, weights, k, (T*)out.at,
-                  out.stride, d);
+    const Deal d = deal<T, N>(t, c, 2);
+#define FG_COMBINE(WEIGHTED, STREAM) \
+    FG_LAUNCH_DEAL(2, d, kMostBlocks, stream, FG_COMBINE_OF(WEIGHTED, STREAM), (const T*)rows.at, rows.stride, (uint32_t)n_rows, index, weights, k, (T*)out.at, out.stride, d)
+#define FG_COMBINE_OF(WEIGHTED, STREAM) k_combine<T, N, WEIGHTED, STREAM
+    const bool past = ((n_rows < t * k ? n_rows : t * k) + t) * c * (int64_t)sizeof(T) >= kStream;
+    if (weights) { if (past) FG_COMBINE(true, true); else FG_COMBINE(true, false); }
+    else if (past) FG_COMBINE(false, true);
+    else FG_COMBINE(false, false);
+#undef FG_COMBINE_OF
+#undef FG_COMBINE
     return hipSuccess;
 }
 
@@ -649,13 +723,14 @@ hipError_t combine_grad(RowsIn grad_out, int64_t t, int64_t c, RowsIn rows, int6
     // a wavefront or less for a token; more, so that a row is one trip to memory, while the chip has room for it
     int lanes = (int)lanes_for(pieces < 64 ? pieces : 64);
     while (lanes < kBlock && lanes < pieces && lanes * t <= kFill) lanes *= 2;
-    const dim3 grid(blocks_for(t, kBlock / lanes));
+    const dim3 grid = blocks_for(t, kBlock / lanes);
 #define FG_COMBINE_GRAD(WAVES)                                                                                                                  \
     FG_LAUNCH((k_combine_grad<T, N, ROWS, WEIGHTED, WAVES>), grid, dim3(kBlock), 0, stream, (const T*)grad_out.at, grad_out.stride, t, (int32_t)c, \
               (const T*)rows.at, rows.stride, (uint32_t)n_rows, index, weights, k, (T*)grad_rows.at, grad_rows.stride, grad_weights, lanes)
     if (lanes == 256) FG_COMBINE_GRAD(4);
     else if (lanes == 128) FG_COMBINE_GRAD(2);
-    else FG_COMBINE_GRAD(1);
+    else if (lanes == 64) FG_COMBINE_GRAD(1);
+    else FG_COMBINE_GRAD(0);
 #undef FG_COMBINE_GRAD
     return hipSuccess;
 }
@@ -734,11 +809,15 @@ bool sums_with_products(int32_t type, int64_t c)
 
 hipError_t launch_row_sums(const RowSums& r, hipStream_t stream)
 {
-    SumArgs a;
+    SumArgs a = {};
     a.index = r.index; a.order = r.order; a.bounds = r.bounds; a.weights = r.weights; a.grad_weights = r.grad_weights;
-    a.m = (int32_t)r.m; a.n_rows = r.n_rows; a.fan = r.fan; a.by_fan = Divide((uint32_t)r.fan); a.scale = r.scale;
-    if (r.out_type == FG_F32) {
-        FG_BY_TYPE(r.type, r.c, (row_sums_of<T, N, float>(r, a, stream)))
+    a.m = (int32_t)r.m; a.n_rows = r.n_rows; a.by_fan = Divide((uint32_t)r.fan); a.scale = r.scale;
+    if (r.out_type == FG_F32 && r.type != FG_F32) {
+        // pieces of 16 bytes of the output, most of what moves where a table is large
+        if (r.type == FG_BF16)
+            return r.c >= kWide<float> ? row_sums_of<__bf16, kWide<float>, float>(r, a, stream) : row_sums_of<__bf16, 1, float>(r, a, stream);
+        if (r.type == FG_F16)
+            return r.c >= kWide<float> ? row_sums_of<_Float16, kWide<float>, float>(r, a, stream) : row_sums_of<_Float16, 1, float>(r, a, stream);
     }
     FG_BY_TYPE(r.type, r.c, (row_sums_of<T, N, T>(r, a, stream)))
 }
