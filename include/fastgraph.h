@@ -258,8 +258,9 @@ fg_status fg_oc_helper(const int32_t* asso_idx, const int32_t* unique_idx, const
  *
  * Rows are c elements of one type; `*_stride` is the number of elements from a row to the next (outputs: >= c, inputs: any, 0
  * too; what lies between two rows is neither read nor written).  Pointers need the alignment of an element.  Weights are float32.  An index entry outside
- * 0..n_rows-1 (a neighbour list's padding, -1) names no row.  Sums are float32, in the order of the index's entries, and
- * rounded once to the type of the output: the same bits in every run.  Outputs must not overlap inputs.
+ * 0..n_rows-1 (a neighbour list's padding, -1) names no row.  Sums are float32, in an order that goes by the
+ * index, the sizes and the outputs asked for, and rounded once to the type of the output: the same call gives the same bits.
+ * Outputs must not overlap inputs.
  *   1 <= c <= FG_MAX_C, strides <= FG_MAX_STRIDE, 1 <= k <= FG_MAX_K; rows, index entries (t * k) <= FG_MAX_N
  * Errors besides those of the other calls: FG_ERR_UNSUPPORTED for an unknown type or a pointer that an element of its type
  * may not have.  The sorted form of an index (order, bounds) must be fg_index_sort's of that index with that n_rows. */

@@ -13,9 +13,10 @@ namespace {
 constexpr int kMaxBits = 10;                 // of a digit: counters of a wavefront stay below 4 KiB of LDS
 constexpr int kSmallBlock = 1024;
 constexpr int64_t kSmallM = 8192;            // entries that one workgroup sorts in LDS
-constexpr int64_t kSmallRows = 4096;         // rows whose bounds that workgroup writes too
+constexpr int64_t kSmallRows = 1024;         // rows whose bounds a workgroup writes: for more, more workgroups sort the same entries
 constexpr int kBlock = 256;
 constexpr unsigned kXcds = 8;
+constexpr int64_t kSmallBlocks = 256;
 constexpr int kItems = 4;                    // a tile: kBlock x kItems entries, or beyond kMediumM
 constexpr int64_t kMediumM = 1 << 20;
 constexpr int kLargeBlock = 512, kLargeItems = 8;
@@ -108,10 +109,10 @@ __device__ __forceinline__ W block_prefix(W x, W* sums)
 
 // ---- one workgroup -----------------------------------------------------------------------------------------------------
 
+// (of a large table every workgroup sorts all entries: the search of its share of the bounds finds them in LDS, and nothing is launched after it)
 template <int ITEMS>
 __global__ __launch_bounds__(kSmallBlock) void k_sort_small(const int32_t* __restrict__ index, int32_t m, uint32_t n_rows, int bits, int passes,
-                                                            int32_t* __restrict__ order, int32_t* __restrict__ place, int32_t* __restrict__ bounds,
-                                                            uint32_t* __restrict__ keys_out)
+                                                            int32_t* __restrict__ order, int32_t* __restrict__ place, int32_t* __restrict__ bounds)
 {
     constexpr int kW = kSmallBlock / 64;
     __shared__ uint32_t keys[ITEMS * kSmallBlock], from[ITEMS * kSmallBlock];
@@ -167,21 +168,20 @@ __global__ __launch_bounds__(kSmallBlock) void k_sort_small(const int32_t* __res
             }
         }
     }
+    if (blockIdx.x == 0)
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        const int e = (wave * ITEMS + i) * 64 + lane;
-        if (e < m) {
-            order[e] = at[i];
-            if (place) place[at[i]] = key[i] < n_rows ? e : -1;
-            if (keys_out) keys_out[e] = key[i];
+        for (int i = 0; i < ITEMS; ++i) {
+            const int e = (wave * ITEMS + i) * 64 + lane;
+            if (e < m) {
+                order[e] = at[i];
+                if (place) place[at[i]] = key[i] < n_rows ? e : -1;
+            }
         }
-    }
-    if (keys_out) return;                                    // many rows: k_sort_bounds
-    for (uint32_t v = tid; v <= n_rows; v += kSmallBlock) {
+    for (int64_t v = (int64_t)blockIdx.x * kSmallBlock + tid; v <= n_rows; v += (int64_t)gridDim.x * kSmallBlock) {
         int lo = 0, hi = m;
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;
-            if (keys[mid] < v) lo = mid + 1; else hi = mid;
+            if (keys[mid] < (uint32_t)v) lo = mid + 1; else hi = mid;
         }
         bounds[v] = lo;
     }
@@ -401,12 +401,11 @@ hipError_t many(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, 
 }
 
 template <int ITEMS>
-hipError_t small(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, int32_t* order, int32_t* place, int32_t* bounds, void* workspace,
-                 hipStream_t stream)
+hipError_t small(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, int32_t* order, int32_t* place, int32_t* bounds, hipStream_t stream)
 {
-    uint32_t* keys = n_rows > kSmallRows ? (uint32_t*)workspace : nullptr;
-    FG_LAUNCH(k_sort_small<ITEMS>, dim3(1), dim3(kSmallBlock), 0, stream, index, (int32_t)m, (uint32_t)n_rows, p.bits, p.passes, order, place, bounds, keys);
-    if (keys) FG_LAUNCH(k_sort_bounds, dim3((unsigned)(n_rows / kBlock + 1)), dim3(kBlock), 0, stream, keys, (int32_t)m, n_rows, bounds);
+    const int64_t blocks = (n_rows + kSmallRows) / kSmallRows;
+    FG_LAUNCH(k_sort_small<ITEMS>, dim3((unsigned)(blocks < kSmallBlocks ? blocks : kSmallBlocks)), dim3(kSmallBlock), 0, stream, index, (int32_t)m,
+              (uint32_t)n_rows, p.bits, p.passes, order, place, bounds);
     return hipSuccess;
 }
 
@@ -414,7 +413,7 @@ hipError_t small(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p,
 
 size_t index_sort_workspace_bytes(int64_t m, int64_t n_rows)
 {
-    if (takes_small_sort(m)) return n_rows > kSmallRows ? up((size_t)m * 4) : 0;
+    if (takes_small_sort(m)) return 0;
     return layout_for(m, plan_for(m, n_rows)).total;
 }
 
@@ -423,9 +422,9 @@ hipError_t launch_index_sort(const int32_t* index, int64_t m, int64_t n_rows, in
 {
     const Plan p = plan_for(m, n_rows);
     if (takes_small_sort(m)) {
-        if (m <= kSmallBlock) return small<1>(index, m, n_rows, p, order, place, bounds, workspace, stream);
-        if (m <= 2 * kSmallBlock) return small<2>(index, m, n_rows, p, order, place, bounds, workspace, stream);
-        return small<8>(index, m, n_rows, p, order, place, bounds, workspace, stream);
+        if (m <= kSmallBlock) return small<1>(index, m, n_rows, p, order, place, bounds, stream);
+        if (m <= 2 * kSmallBlock) return small<2>(index, m, n_rows, p, order, place, bounds, stream);
+        return small<8>(index, m, n_rows, p, order, place, bounds, stream);
     }
     if (!p.large) return many<kBlock, kItems>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);
     return many<kLargeBlock, kLargeItems>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);

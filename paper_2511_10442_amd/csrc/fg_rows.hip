@@ -392,7 +392,7 @@ __global__ __launch_bounds__(kBlock, ROWS ? 3 : 4) void k_combine_grad(const T* 
 //   k_row_sums   chunks of one row each: their sums; rows without such a chunk: from their entries
 //   k_row_parts  chunks of chunks (where there are enough entries)
 //   k_row_join   rows with a chunk: the entries before it, chunks up to the first whole chunk of chunks, those, and so back
-// The long rows' entries are read while the many short ones are written.
+// The long rows' entries are read while the many short ones are written.  Few entries and rows: k_row_sums_few alone, a launch instead of two or three.
 constexpr int kChunk = 32, kChunks = 32;
 constexpr int64_t kPartsFrom = 16;           // chunks of chunks from which on it is looked whether there are any
 
@@ -486,10 +486,9 @@ __device__ __forceinline__ bool one_row(const SumArgs& a, int32_t p, int32_t n, 
     return name == a.index[e1] && (uint32_t)name < (uint32_t)a.n_rows;
 }
 
-__device__ __forceinline__ void range_of(const SumArgs& a, int64_t row, int32_t& from, int32_t& to)
+// (bounds that are no fg_index_sort's: nothing outside is read)
+__device__ __forceinline__ void within(const SumArgs& a, int32_t& from, int32_t& to)
 {
-    from = a.bounds[row];
-    to = a.bounds[row + 1];
     from = from < 0 ? 0 : from;
     to = to > a.m ? a.m : to;
 }
@@ -530,31 +529,83 @@ __global__ __launch_bounds__(kBlock, DOTS && sizeof(T) == 2 ? 3 : 4) void k_row_
     a.index = index; a.order = order; a.bounds = bounds; a.weights = weights;        // (arguments of their own: nothing stored changes them)
     each_span<N, SEGS>(d, [&](const Span<S>& at) {
         const bool real = !DOTS || at.skip[0] < N;
-        const bool is_chunk = at.row < a.chunks;
-        int64_t name = at.row - a.chunks;
-        int32_t from, to;
-        if (is_chunk) {
-            int32_t of;
-            from = (int32_t)at.row << a.shift;
-            to = from + (1 << a.shift);
-            if (!one_row(a, from, 1 << a.shift, of)) return;
-            name = of;
-        } else {
-            range_of(a, name, from, to);
-            if (first_chunk(a, from) < to >> a.shift) return;              // k_row_join
-            if (ACCUMULATE && from >= to) return;
-        }
-        typename P::Wide sum[S] = {}, row = {};
-        if (DOTS && from < to) row = wide<T, N>(load_piece<T, N>(rows + name * rows_stride + at.col[0]));
-        add_entries<T, N, WEIGHTED, DOTS, S>(sum, a, grad, grad_stride, from, to, at, row, real, (int)d.pieces);
-        if (is_chunk) {
+        if (at.row < a.chunks) {
+            int32_t name;
+            const int32_t from = (int32_t)at.row << a.shift, n = 1 << a.shift;
+            if (!one_row(a, from, n, name)) return;
+            typename P::Wide sum[S] = {}, row = {};
+            if (DOTS) row = wide<T, N>(load_piece<T, N>(rows + (int64_t)name * rows_stride + at.col[0]));
+            add_entries<T, N, WEIGHTED, DOTS, S>(sum, a, grad, grad_stride, from, from + n, at, row, real, (int)d.pieces);
 #pragma unroll
             for (int s = 0; s < S; ++s)
                 if (real && at.there[s]) *reinterpret_cast<typename P::Wide*>(a.parts + (at.row * d.pieces + at.piece[s]) * N) = sum[s];
-        } else {
-            store_sum<T, N, TO, ACCUMULATE, STREAM, S>(a, sum, out, out_stride, name, at);
+            return;
         }
+        const int64_t name = at.row - a.chunks;
+        int32_t from = a.bounds[name], to = a.bounds[name + 1];
+        within(a, from, to);
+        if (first_chunk(a, from) < to >> a.shift) return;                  // k_row_join
+        if (ACCUMULATE && from >= to) return;
+        typename P::Wide sum[S] = {}, row = {};
+        if (DOTS && from < to) row = wide<T, N>(load_piece<T, N>(rows + name * rows_stride + at.col[0]));
+        add_entries<T, N, WEIGHTED, DOTS, S>(sum, a, grad, grad_stride, from, to, at, row, real, (int)d.pieces);
+        store_sum<T, N, TO, ACCUMULATE, STREAM, S>(a, sum, out, out_stride, name, at);
     });
+}
+
+// Few entries and rows: a wavefront for 64 pieces of a row; where a row has more than kAlone entries, the workgroup's wavefronts take a share of them each and meet in LDS.
+constexpr int kFewBlock = 1024, kAlone = 32;
+constexpr int64_t kFewEntries = 8192, kFewUnits = 32768;
+template <typename T, int N, typename TO, bool WEIGHTED, bool ACCUMULATE>
+__global__ __launch_bounds__(kFewBlock) void k_row_sums_few(SumArgs a, const int32_t* __restrict__ order, const int32_t* __restrict__ bounds,
+                                                            const float* __restrict__ weights, const T* __restrict__ grad, int64_t grad_stride,
+                                                            TO* __restrict__ out, int64_t out_stride, Deal d)
+{
+    constexpr int kW = kFewBlock / 64;
+    typedef typename Piece<T, N>::Wide Wide;
+    __shared__ int32_t range[kW][2];
+    __shared__ Wide part[kW][64];
+    a.order = order; a.bounds = bounds; a.weights = weights;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    auto span = [&](int w, int64_t& row) {
+        const int64_t unit = (int64_t)blockIdx.x * kW + w;
+        row = d.by_waves_far(unit);
+        return span_of<N, 1>(d, row, (uint32_t)(unit - row * d.waves) * 64 + lane);
+    };
+    int64_t row;
+    const Span<1> at = span(wave, row);
+    int32_t from = 0, to = 0;
+    const bool there = row < a.n_rows;
+    if (there) {
+        from = bounds[row];
+        to = bounds[row + 1];
+        within(a, from, to);
+    }
+    if (lane == 0) { range[wave][0] = from; range[wave][1] = to; }
+    if (there && to - from <= kAlone && !(ACCUMULATE && from >= to)) {
+        Wide sum[1] = {}, none = {};
+        add_entries<T, N, WEIGHTED, false, 1>(sum, a, grad, grad_stride, from, to, at, none, true, 0);
+        store_sum<T, N, TO, ACCUMULATE, false, 1>(a, sum, out, out_stride, row, at);
+    }
+    __syncthreads();
+    for (int w = 0; w < kW; ++w) {
+        const int32_t f = range[w][0], n = range[w][1] - f;
+        if (n <= kAlone) continue;
+        const int32_t share = (n + kW - 1) / kW, mine = wave * share < n ? wave * share : n, end = mine + share < n ? mine + share : n;
+        int64_t of;
+        const Span<1> there_at = span(w, of);
+        Wide sum[1] = {}, none = {};
+        add_entries<T, N, WEIGHTED, false, 1>(sum, a, grad, grad_stride, f + mine, f + end, there_at, none, true, 0);
+        part[wave][lane] = sum[0];
+        __syncthreads();
+        if (wave == w) {
+            sum[0] = part[0][lane];
+#pragma unroll
+            for (int i = 1; i < kW; ++i) sum[0] += part[i][lane];
+            store_sum<T, N, TO, ACCUMULATE, false, 1>(a, sum, out, out_stride, row, at);
+        }
+        __syncthreads();
+    }
 }
 
 template <typename T, int N>
@@ -574,11 +625,21 @@ __global__ __launch_bounds__(kBlock) void k_row_join(SumArgs a, const T* __restr
                                                      int64_t rows_stride, TO* __restrict__ out, int64_t out_stride, Deal d)
 {
     typedef Piece<T, N> P;
+    if (DOTS) {
+        // weights' gradients of entries that name no row
+        int64_t p = a.bounds[a.n_rows];
+        for (p = (p < 0 ? 0 : p) + (int64_t)blockIdx.x * kBlock + threadIdx.x; p < a.m; p += (int64_t)gridDim.x * kBlock) {
+            const uint32_t e = (uint32_t)a.order[p];
+            if (e < (uint32_t)a.m) a.grad_weights[e] = 0.0f;
+        }
+    }
     each_span<N, 0>(d, [&](const Span<1>& at) {
         int32_t name, from, to;
         const int32_t q0 = (int32_t)at.row;
         if (!one_row(a, q0 << a.shift, 1 << a.shift, name)) return;
-        range_of(a, name, from, to);
+        from = a.bounds[name];
+        to = a.bounds[name + 1];
+        within(a, from, to);
         const int32_t q1 = to >> a.shift;
         if (first_chunk(a, from) != q0 || q0 >= q1) return;                // the row's first chunk has the row
         const bool real = !DOTS || at.skip[0] < N;
@@ -604,17 +665,6 @@ __global__ __launch_bounds__(kBlock) void k_row_join(SumArgs a, const T* __restr
     });
 }
 
-// Weights' gradients of entries that name no row.
-__global__ __launch_bounds__(kBlock) void k_no_rows(SumArgs a)
-{
-    int64_t p = a.bounds[a.n_rows];
-    p = (p < 0 ? 0 : p) + (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    for (; p < a.m; p += (int64_t)gridDim.x * kBlock) {
-        const uint32_t e = (uint32_t)a.order[p];
-        if (e < (uint32_t)a.m) a.grad_weights[e] = 0.0f;
-    }
-}
-
 // lanes that take a row's pieces where they have to meet: a power of two from 8 on
 inline uint32_t lanes_for(int64_t pieces)
 {
@@ -632,34 +682,41 @@ hipError_t row_sums(const RowSums& r, const SumArgs& a, hipStream_t stream)
     uint32_t pieces = (uint32_t)((r.c + N - 1) / N);
     if (DOTS) pieces = lanes_for(pieces);
     SumArgs b = a;
+    if constexpr (!DOTS) {
+        Deal d = deal(r.n_rows, r.c, pieces, 1);
+        d.waves = (pieces + 63) / 64;                        // a wavefront for 64 pieces whatever the width
+        d.by_waves_far = DivideFar(d.waves);
+        d.units = r.n_rows * d.waves;
+        if (r.m <= kFewEntries && d.units <= kFewUnits) {
+            FG_LAUNCH((k_row_sums_few<T, N, TO, WEIGHTED, ACCUMULATE>), blocks_for(d.units, kFewBlock / 64), dim3(kFewBlock), 0, stream, b, b.order, b.bounds,
+                      b.weights, grad, r.grad.stride, (TO*)r.out.at, r.out.stride, d);
+            return hipSuccess;
+        }
+    }
     int64_t chunk = kChunk;
     b.shift = 5;
     while (r.n_rows * pieces >= kFill && chunk < 4 * (r.m / r.n_rows) && chunk < 65536) { chunk *= 2; ++b.shift; }
     b.chunks = r.m / chunk;
     b.parts = r.partials;
     b.parts2 = nullptr;
-    const Deal d = deal(b.chunks + r.n_rows, r.c, pieces, DOTS ? 1 : 4);
+    const Deal d = deal(b.chunks + r.n_rows, r.c, pieces, DOTS ? 1 : 2);
 #define FG_SUMS(STREAM) k_row_sums<T, N, TO, WEIGHTED, ACCUMULATE, DOTS, STREAM
 #define FG_SUMS_ARGS b, b.index, b.order, b.bounds, b.weights, grad, r.grad.stride, rows, r.rows.stride, (TO*)r.out.at, r.out.stride, d
-    if constexpr (DOTS) {
-        FG_LAUNCH_DEAL(1, d, kMostUneven, stream, FG_SUMS(false), FG_SUMS_ARGS);
-        FG_LAUNCH(k_no_rows, blocks_for((r.m + 15) / 16, kBlock), dim3(kBlock), 0, stream, b);
-    } else if (ACCUMULATE || (r.n_rows * (int64_t)sizeof(TO) + r.m / r.fan * (int64_t)sizeof(T)) * r.c < kStream) {
-        FG_LAUNCH_DEAL(4, d, kMostUneven, stream, FG_SUMS(false), FG_SUMS_ARGS);
-    } else {
-        FG_LAUNCH_DEAL(4, d, kMostUneven, stream, FG_SUMS(!ACCUMULATE), FG_SUMS_ARGS);
-    }
+    const bool past = !ACCUMULATE && !DOTS && (r.n_rows * (int64_t)sizeof(TO) + r.m / r.fan * (int64_t)sizeof(T)) * r.c >= kStream;
+    if constexpr (DOTS) FG_LAUNCH_DEAL(1, d, kMostUneven, stream, FG_SUMS(false), FG_SUMS_ARGS);
+    else if (!past) FG_LAUNCH_DEAL(2, d, kMostUneven, stream, FG_SUMS(false), FG_SUMS_ARGS);
+    else FG_LAUNCH_DEAL(2, d, kMostUneven, stream, FG_SUMS(!ACCUMULATE), FG_SUMS_ARGS);
 #undef FG_SUMS_ARGS
 #undef FG_SUMS
-    if (!b.chunks) return hipSuccess;
+    if (!b.chunks && !DOTS) return hipSuccess;
     if (b.chunks / kChunks >= kPartsFrom) {
         b.parts2 = r.partials + b.chunks * ((int64_t)pieces * N);
         const Deal dp = deal(b.chunks / kChunks, r.c, pieces, 0);
         FG_LAUNCH((k_row_parts<T, N>), blocks_for(dp.total, kBlock), dim3(kBlock), 0, stream, b, dp);
     }
     const Deal dj = deal(b.chunks, r.c, pieces, 0);
-    FG_LAUNCH((k_row_join<T, N, TO, WEIGHTED, ACCUMULATE, DOTS>), blocks_for(dj.total, kBlock), dim3(kBlock), 0, stream, b, grad, r.grad.stride, rows,
-              r.rows.stride, (TO*)r.out.at, r.out.stride, dj);
+    FG_LAUNCH((k_row_join<T, N, TO, WEIGHTED, ACCUMULATE, DOTS>), blocks_for(dj.total > 0 ? dj.total : 1, kBlock), dim3(kBlock), 0, stream, b, grad,
+              r.grad.stride, rows, r.rows.stride, (TO*)r.out.at, r.out.stride, dj);
     return hipSuccess;
 }
 

@@ -312,12 +312,15 @@ def test_shared_rows(n, t, k, c, dtype):
     by = B.fg_index_sort(dev(index), n)
     for weights in (w, None):
         wide = None if weights is None else R.wide(w)
-        gw = torch.full((t, k), 7.0, device=DEV)
+        gw, again = torch.full((t, k), 7.0, device=DEV), torch.full((t, k), 7.0, device=DEV)
         got, gw = B.fg_combine_backward(grad, rows, dev(index), weights, sort=by, grad_weights=gw)
         ref, mass, count = R.row_sums(R.wide(grad), index, wide, n)
         R.check(got, ref, mass, count[:, None], dtype)
         R.check(gw, *R.dots(R.wide(grad), R.wide(rows), index), c, torch.float32)
-        assert torch.equal(got, B.fg_combine_backward(grad, rows, dev(index), weights, sort=by)[0])
+        # the same call, the same bits
+        assert all(torch.equal(a, b) for a, b in zip((got, gw), B.fg_combine_backward(grad, rows, dev(index), weights, sort=by, grad_weights=again)))
+        if weights is None:                                                  # without the weights' gradient it is another kernel's
+            R.check(B.fg_combine_backward(grad, rows, dev(index), sort=by)[0], ref, mass, count[:, None], dtype)
     ref, mass = R.combine(R.wide(rows), index, R.wide(w))
     R.check(B.fg_combine(rows, dev(index), w), ref, mass, k, dtype)
 
