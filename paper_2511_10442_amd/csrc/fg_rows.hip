@@ -29,9 +29,14 @@ struct Piece {
     static constexpr int kWords = N * (int)sizeof(T) / 4;
     typedef uint32_t Words __attribute__((ext_vector_type(kWords < 1 ? 1 : kWords)));
 };
-template <typename T, int N>
-__device__ __forceinline__ typename Piece<T, N>::Vec load_piece(const T* __restrict__ p) { return *reinterpret_cast<const typename Piece<T, N>::Vec*>(p); }
-// STREAM: past the caches, where nobody would find it there (kStream).  A template argument: of two stores behind a test the compiler makes one
+// STREAM: past the caches, where nobody would find it again (kStream).  A template argument: of two accesses behind a test the compiler makes one
+template <typename T, int N, bool STREAM = false>
+__device__ __forceinline__ typename Piece<T, N>::Vec load_piece(const T* __restrict__ p)
+{
+    const auto* at = reinterpret_cast<const typename Piece<T, N>::Vec*>(p);
+    if constexpr (STREAM) return __builtin_nontemporal_load(at);
+    else return *at;
+}
 template <bool STREAM, typename V, typename T>
 __device__ __forceinline__ void store_vec(T* __restrict__ p, V v)
 {
@@ -262,7 +267,7 @@ __global__ __launch_bounds__(kBlock) void k_combine(const T* __restrict__ rows, 
             for (int u = 0; u < U; ++u) {
                 const bool named = u < there && (uint32_t)name[u] < n_rows;
 #pragma unroll
-                for (int s = 0; s < S; ++s) v[u][s] = load_piece<T, N>(rows + (named ? (int64_t)name[u] : 0) * rows_stride + at.col[s]);
+                for (int s = 0; s < S; ++s) v[u][s] = load_piece<T, N, STREAM>(rows + (named ? (int64_t)name[u] : 0) * rows_stride + at.col[s]);
                 if (WEIGHTED) w[u] = named ? w[u] : 0.0f;
                 name[u] = named;
             }
@@ -283,15 +288,17 @@ __global__ __launch_bounds__(kBlock) void k_combine(const T* __restrict__ rows, 
 
 // ---- gradients of weights, and of rows that are named once -------------------------------------------------------------
 
-// Adds eight values over `lanes` lanes of a wavefront (a power of two from 8 on; the lane's number among them is `lane`): at each of three steps a lane
-// hands half of its values to the lane opposite and takes the other half, then the one that is left is added up.  Returns the sum of value
-// eighth(lane, lanes).
-__device__ __forceinline__ int eighth(int lane, int lanes) { return lane >> (__builtin_ctz(lanes) - 3); }
-__device__ __forceinline__ float add_eight(float (&x)[8], int lane, int lanes)
+// Adds U values (8, 4, 2 or 1) over `lanes` lanes of a wavefront (a power of two from 8 on; the lane's number among them is `lane`): at each of log U steps
+// a lane hands half of its values to the lane opposite and takes the other half, then the one that is left is added up.  Returns the sum of value
+// share_of<U>(lane, lanes).
+template <int U>
+__device__ __forceinline__ int share_of(int lane, int lanes) { return lane >> (__builtin_ctz(lanes) - __builtin_ctz(U)); }
+template <int U>
+__device__ __forceinline__ float add_up(float (&x)[U], int lane, int lanes)
 {
     int o = lanes >> 1;
 #pragma unroll
-    for (int half = 4; half > 0; half >>= 1, o >>= 1) {
+    for (int half = U / 2; half > 0; half >>= 1, o >>= 1) {
         const bool upper = lane & o;
 #pragma unroll
         for (int u = 0; u < half; ++u) {
@@ -306,7 +313,7 @@ __device__ __forceinline__ float add_eight(float (&x)[8], int lane, int lanes)
 
 // `lanes` lanes (8 to 32: WAVES == 0; 64, 128 or 256: WAVES wavefronts, which meet in LDS) take a token: they walk along its row and those of up
 // to eight of its k, so that the token's gradient is loaded once for the eight.
-template <typename T, int N, bool ROWS, bool WEIGHTED, int WAVES>
+template <typename T, int N, bool ROWS, bool WEIGHTED, bool STREAM, int WAVES>
 __global__ __launch_bounds__(kBlock, ROWS ? 3 : 4) void k_combine_grad(const T* __restrict__ grad_out, int64_t grad_stride, int64_t t, int32_t c,
                                                          const T* __restrict__ rows, int64_t rows_stride, uint32_t n_rows,
                                                          const int32_t* __restrict__ index, const float* __restrict__ weights, int32_t k,
@@ -324,51 +331,48 @@ __global__ __launch_bounds__(kBlock, ROWS ? 3 : 4) void k_combine_grad(const T* 
         const int64_t row = turn * each + group;
         const bool there = row < t;
         const int64_t base = there ? row * k : 0;
-        for (int32_t j0 = 0; j0 < k; j0 += 8) {
-            int32_t name[8];
-            float w[8], dot[8];
-            load_words<8>(index + base + j0, k - j0, name);
-            if (WEIGHTED) load_words<8>(weights + base + j0, k - j0, w);
+        in_chunks<8>(k, [&](auto count, int32_t j, int here) {
+            constexpr int U = count.value;
+            int32_t name[U];
+            float w[U], dot[U];
+            load_words<U>(index + base + j, here, name);
+            if (WEIGHTED) load_words<U>(weights + base + j, here, w);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                if (j0 + u >= k || (uint32_t)name[u] >= n_rows) name[u] = -1;
+            for (int u = 0; u < U; ++u) {
+                if (u >= here || (uint32_t)name[u] >= n_rows) name[u] = -1;
                 dot[u] = 0.0f;
             }
             for (int32_t turn_col = lane * N; there && turn_col < c; turn_col += lanes * N) {
                 const int32_t col = turn_col > c - N ? c - N : turn_col, skip = turn_col - col;
                 const typename P::Wide g = wide<T, N>(load_piece<T, N>(grad_out + row * grad_stride + col));
                 if (dots) {
-                    typename P::Vec v[8];
+                    typename P::Vec v[U];
 #pragma unroll
-                    for (int u = 0; u < 8; ++u)
-                        if (u == 0 || j0 + u < k)
-                            v[u] = load_piece<T, N>(rows + (name[u] < 0 ? 0 : (int64_t)name[u]) * rows_stride + col);
+                    for (int u = 0; u < U; ++u) v[u] = load_piece<T, N, STREAM>(rows + (name[u] < 0 ? 0 : (int64_t)name[u]) * rows_stride + col);
 #pragma unroll
-                    for (int u = 0; u < 8; ++u)
-                        if (u == 0 || j0 + u < k) {
-                            const typename P::Wide x = wide<T, N>(v[u]);
+                    for (int u = 0; u < U; ++u) {
+                        const typename P::Wide x = wide<T, N>(v[u]);
 #pragma unroll
-                            for (int i = 0; i < N; ++i)
-                                if (i >= skip) dot[u] = __builtin_fmaf(x[i], g[i], dot[u]);
-                        }
+                        for (int i = 0; i < N; ++i)
+                            if (i >= skip) dot[u] = __builtin_fmaf(x[i], g[i], dot[u]);
+                    }
                 }
                 if constexpr (ROWS)
 #pragma unroll
-                    for (int u = 0; u < 8; ++u)
+                    for (int u = 0; u < U; ++u)
                         if (name[u] >= 0) {
                             float by = WEIGHTED ? w[u] : 1.0f;
-                            if (WEIGHTED) asm volatile("" : "+v"(by));       // eight rows' products would otherwise be made ahead, in 64 registers
-                            store_piece<T, N>(grad_rows + (int64_t)name[u] * grad_rows_stride + col, narrow<T, N>(WEIGHTED ? g * by : g));
+                            if (WEIGHTED) asm volatile("" : "+v"(by));       // the rows' products would otherwise be made ahead, in 64 registers
+                            store_piece<T, N, STREAM>(grad_rows + (int64_t)name[u] * grad_rows_stride + col, narrow<T, N>(WEIGHTED ? g * by : g));
                         }
             }
-            if (!grad_weights) continue;
+            if (!grad_weights) return;
             // (products with row 0, of entries that name none, are dropped here, NaN and all)
 #pragma unroll
-            for (int u = 0; u < 8; ++u) dot[u] = name[u] < 0 ? 0.0f : dot[u];
-            const int some = WAVES ? 64 : lanes;
-            float sum = add_eight(dot, threadIdx.x & (some - 1), some);
-            const int u = eighth(threadIdx.x & (some - 1), some);
-            bool writes = (threadIdx.x & (some / 8 - 1)) == 0;
+            for (int u = 0; u < U; ++u) dot[u] = name[u] < 0 ? 0.0f : dot[u];
+            const int some = WAVES ? 64 : lanes, at = threadIdx.x & (some - 1), u = share_of<U>(at, some);
+            float sum = add_up<U>(dot, at, some);
+            bool writes = (at & (some / U - 1)) == 0;
             if constexpr (WAVES > 1) {
                 const int wave = threadIdx.x >> 6;
                 if (writes) part[wave][u] = sum;
@@ -379,8 +383,8 @@ __global__ __launch_bounds__(kBlock, ROWS ? 3 : 4) void k_combine_grad(const T* 
                     for (int o = 1; o < WAVES; ++o) sum += part[wave + o][u];
                 __syncthreads();
             }
-            if (writes && there && j0 + u < k) grad_weights[base + j0 + u] = sum;
-        }
+            if (writes && there && u < here) grad_weights[base + j + u] = sum;
+        });
     }
 }
 
@@ -389,9 +393,9 @@ __global__ __launch_bounds__(kBlock, ROWS ? 3 : 4) void k_combine_grad(const T* 
 // Rows that are named often are summed in parts: `chunk` entries of the sorted index that all name one row, and kChunks such chunks, are summed
 // by themselves and put together afterwards, so that what one lane does for a row hardly grows with the row's entries.  chunk is kChunk, or where
 // there are rows enough to fill the chip, four times the mean of a row's entries (a power of two): rows of a graph are named often, but all of them.
-//   k_row_sums   chunks of one row each: their sums; rows without such a chunk: from their entries
+//   k_row_sums   chunks of one row each, a row's first and last with its entries before and after them: their sums; rows without such a chunk
 //   k_row_parts  chunks of chunks (where there are enough entries)
-//   k_row_join   rows with a chunk: the entries before it, chunks up to the first whole chunk of chunks, those, and so back
+//   k_row_join   rows with a chunk: chunks up to the first whole chunk of chunks, those, and chunks again
 // The long rows' entries are read while the many short ones are written.  Few entries and rows: k_row_sums_few alone, a launch instead of two or three.
 constexpr int kChunk = 32, kChunks = 32;
 constexpr int64_t kPartsFrom = 16;           // chunks of chunks from which on it is looked whether there are any
@@ -431,7 +435,7 @@ __device__ __forceinline__ void add_entries(typename Piece<T, N>::Wide (&sum)[S]
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int s = 0; s < S; ++s) v[u][s] = load_piece<T, N>(grad + (int64_t)a.by_fan((uint32_t)entry[u]) * grad_stride + at.col[s]);
-        float dot[8];
+        float dot[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (WEIGHTED) w[u] = u < there ? w[u] : 0.0f;
@@ -448,11 +452,9 @@ __device__ __forceinline__ void add_entries(typename Piece<T, N>::Wide (&sum)[S]
             dot[u] = products;
         }
         if constexpr (DOTS) {
-#pragma unroll
-            for (int u = U; u < 8; ++u) dot[u] = 0.0f;
-            const int lane = threadIdx.x & (lanes - 1), mine = eighth(lane, lanes);
-            const float product = add_eight(dot, lane, lanes);
-            if ((lane & (lanes / 8 - 1)) == 0 && mine < there) {
+            const int lane = threadIdx.x & (lanes - 1), mine = share_of<U>(lane, lanes);
+            const float product = add_up<U>(dot, lane, lanes);
+            if ((lane & (lanes / U - 1)) == 0 && mine < there) {
                 const uint32_t e = (uint32_t)a.order[from + p + mine];
                 if (e < (uint32_t)a.m) a.grad_weights[e] = product;
             }
@@ -530,12 +532,16 @@ __global__ __launch_bounds__(kBlock, DOTS && sizeof(T) == 2 ? 3 : 4) void k_row_
     each_span<N, SEGS>(d, [&](const Span<S>& at) {
         const bool real = !DOTS || at.skip[0] < N;
         if (at.row < a.chunks) {
+            const int32_t q = (int32_t)at.row;
             int32_t name;
-            const int32_t from = (int32_t)at.row << a.shift, n = 1 << a.shift;
-            if (!one_row(a, from, n, name)) return;
+            if (!one_row(a, q << a.shift, 1 << a.shift, name)) return;
+            int32_t from = a.bounds[name], to = a.bounds[name + 1];
+            within(a, from, to);
+            if (first_chunk(a, from) < q) from = q << a.shift;
+            if (to >> a.shift > q + 1) to = (q + 1) << a.shift;
             typename P::Wide sum[S] = {}, row = {};
             if (DOTS) row = wide<T, N>(load_piece<T, N>(rows + (int64_t)name * rows_stride + at.col[0]));
-            add_entries<T, N, WEIGHTED, DOTS, S>(sum, a, grad, grad_stride, from, from + n, at, row, real, (int)d.pieces);
+            add_entries<T, N, WEIGHTED, DOTS, S>(sum, a, grad, grad_stride, from, to, at, row, real, (int)d.pieces);
 #pragma unroll
             for (int s = 0; s < S; ++s)
                 if (real && at.there[s]) *reinterpret_cast<typename P::Wide*>(a.parts + (at.row * d.pieces + at.piece[s]) * N) = sum[s];
@@ -620,13 +626,11 @@ __global__ __launch_bounds__(kBlock) void k_row_parts(SumArgs a, Deal d)
     });
 }
 
-template <typename T, int N, typename TO, bool WEIGHTED, bool ACCUMULATE, bool DOTS>
-__global__ __launch_bounds__(kBlock) void k_row_join(SumArgs a, const T* __restrict__ grad, int64_t grad_stride, const T* __restrict__ rows,
-                                                     int64_t rows_stride, TO* __restrict__ out, int64_t out_stride, Deal d)
+// NONE: and the weights' gradients of entries that name no row
+template <typename T, int N, typename TO, bool ACCUMULATE, bool NONE>
+__global__ __launch_bounds__(kBlock) void k_row_join(SumArgs a, TO* __restrict__ out, int64_t out_stride, Deal d)
 {
-    typedef Piece<T, N> P;
-    if (DOTS) {
-        // weights' gradients of entries that name no row
+    if (NONE) {
         int64_t p = a.bounds[a.n_rows];
         for (p = (p < 0 ? 0 : p) + (int64_t)blockIdx.x * kBlock + threadIdx.x; p < a.m; p += (int64_t)gridDim.x * kBlock) {
             const uint32_t e = (uint32_t)a.order[p];
@@ -634,32 +638,23 @@ __global__ __launch_bounds__(kBlock) void k_row_join(SumArgs a, const T* __restr
         }
     }
     each_span<N, 0>(d, [&](const Span<1>& at) {
-        int32_t name, from, to;
         const int32_t q0 = (int32_t)at.row;
+        int32_t name;
         if (!one_row(a, q0 << a.shift, 1 << a.shift, name)) return;
-        from = a.bounds[name];
-        to = a.bounds[name + 1];
+        int32_t from = a.bounds[name], to = a.bounds[name + 1];
         within(a, from, to);
+        if (first_chunk(a, from) != q0) return;                            // the row's first chunk has the row
         const int32_t q1 = to >> a.shift;
-        if (first_chunk(a, from) != q0 || q0 >= q1) return;                // the row's first chunk has the row
-        const bool real = !DOTS || at.skip[0] < N;
-        typename P::Wide sum[1] = {}, row = {};
-        if (DOTS) row = wide<T, N>(load_piece<T, N>(rows + (int64_t)name * rows_stride + at.col[0]));
         const int64_t stride = (int64_t)d.pieces * N;
         const float *parts = a.parts + at.piece[0] * N, *parts2 = a.parts2 + at.piece[0] * N;
         const int32_t r0 = a.parts2 ? (q0 + kChunks - 1) / kChunks : q1, r1 = a.parts2 ? q1 / kChunks : 0;
-        // (the single entries before and after the chunks in one loop's code)
-#pragma unroll 1
-        for (int side = 0; side < 2; ++side) {
-            add_entries<T, N, WEIGHTED, DOTS, 1>(sum, a, grad, grad_stride, side ? q1 << a.shift : from, side ? to : q0 << a.shift, at, row, real, (int)d.pieces);
-            if (side) break;
-            if (r0 < r1) {
-                add_parts<T, N>(sum[0], parts, stride, q0, r0 * kChunks);
-                add_parts<T, N>(sum[0], parts2, stride, r0, r1);
-                add_parts<T, N>(sum[0], parts, stride, r1 * kChunks, q1);
-            } else {
-                add_parts<T, N>(sum[0], parts, stride, q0, q1);
-            }
+        typename Piece<T, N>::Wide sum[1] = {};
+        if (r0 < r1) {
+            add_parts<T, N>(sum[0], parts, stride, q0, r0 * kChunks);
+            add_parts<T, N>(sum[0], parts2, stride, r0, r1);
+            add_parts<T, N>(sum[0], parts, stride, r1 * kChunks, q1);
+        } else {
+            add_parts<T, N>(sum[0], parts, stride, q0, q1);
         }
         store_sum<T, N, TO, ACCUMULATE, false, 1>(a, sum, out, out_stride, name, at);
     });
@@ -715,8 +710,7 @@ hipError_t row_sums(const RowSums& r, const SumArgs& a, hipStream_t stream)
         FG_LAUNCH((k_row_parts<T, N>), blocks_for(dp.total, kBlock), dim3(kBlock), 0, stream, b, dp);
     }
     const Deal dj = deal(b.chunks, r.c, pieces, 0);
-    FG_LAUNCH((k_row_join<T, N, TO, WEIGHTED, ACCUMULATE, DOTS>), blocks_for(dj.total > 0 ? dj.total : 1, kBlock), dim3(kBlock), 0, stream, b, grad,
-              r.grad.stride, rows, r.rows.stride, (TO*)r.out.at, r.out.stride, dj);
+    FG_LAUNCH((k_row_join<T, N, TO, ACCUMULATE, DOTS>), blocks_for(dj.total > 0 ? dj.total : 1, kBlock), dim3(kBlock), 0, stream, b, (TO*)r.out.at, r.out.stride, dj);
     return hipSuccess;
 }
 
@@ -763,7 +757,7 @@ hipError_t combine(RowsIn rows, int64_t n_rows, int64_t c, const int32_t* index,
 #define FG_COMBINE(WEIGHTED, STREAM) \
     FG_LAUNCH_DEAL(2, d, kMostBlocks, stream, FG_COMBINE_OF(WEIGHTED, STREAM), (const T*)rows.at, rows.stride, (uint32_t)n_rows, index, weights, k, (T*)out.at, out.stride, d)
 #define FG_COMBINE_OF(WEIGHTED, STREAM) k_combine<T, N, WEIGHTED, STREAM
-    const bool past = ((n_rows < t * k ? n_rows : t * k) + t) * c * (int64_t)sizeof(T) >= kStream;
+    const bool past = n_rows >= t * k && (t * k + t) * c * (int64_t)sizeof(T) >= kStream;      // (rows that are named again are worth keeping)
     if (weights) { if (past) FG_COMBINE(true, true); else FG_COMBINE(true, false); }
     else if (past) FG_COMBINE(false, true);
     else FG_COMBINE(false, false);
@@ -781,13 +775,15 @@ hipError_t combine_grad(RowsIn grad_out, int64_t t, int64_t c, RowsIn rows, int6
     int lanes = (int)lanes_for(pieces < 64 ? pieces : 64);
     while (lanes < kBlock && lanes < pieces && lanes * t <= kFill) lanes *= 2;
     const dim3 grid = blocks_for(t, kBlock / lanes);
-#define FG_COMBINE_GRAD(WAVES)                                                                                                                  \
-    FG_LAUNCH((k_combine_grad<T, N, ROWS, WEIGHTED, WAVES>), grid, dim3(kBlock), 0, stream, (const T*)grad_out.at, grad_out.stride, t, (int32_t)c, \
-              (const T*)rows.at, rows.stride, (uint32_t)n_rows, index, weights, k, (T*)grad_rows.at, grad_rows.stride, grad_weights, lanes)
-    if (lanes == 256) FG_COMBINE_GRAD(4);
-    else if (lanes == 128) FG_COMBINE_GRAD(2);
-    else if (lanes == 64) FG_COMBINE_GRAD(1);
-    else FG_COMBINE_GRAD(0);
+#define FG_COMBINE_GRAD(STREAM, WAVES)                                                                                                             \
+    FG_LAUNCH((k_combine_grad<T, N, ROWS, WEIGHTED, STREAM, WAVES>), grid, dim3(kBlock), 0, stream, (const T*)grad_out.at, grad_out.stride, t,      \
+              (int32_t)c, (const T*)rows.at, rows.stride, (uint32_t)n_rows, index, weights, k, (T*)grad_rows.at, grad_rows.stride, grad_weights, lanes)
+    constexpr bool kOnce = ROWS && N > 1;                     // (ROWS: no row is named twice)
+    if (lanes == 256) FG_COMBINE_GRAD(false, 4);
+    else if (lanes == 128) FG_COMBINE_GRAD(false, 2);
+    else if (lanes == 64 && kOnce && (2 * t * k + t) * c * (int64_t)sizeof(T) >= kStream) FG_COMBINE_GRAD(kOnce, 1);
+    else if (lanes == 64) FG_COMBINE_GRAD(false, 1);
+    else FG_COMBINE_GRAD(false, 0);
 #undef FG_COMBINE_GRAD
     return hipSuccess;
 }
