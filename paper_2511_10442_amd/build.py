@@ -39,7 +39,7 @@ def units():
     """(source, object, extra flags)"""
     out = [(os.path.join(CSRC, f + ".hip"), os.path.join(OBJ, f + ".o"), [])
            for f in ("fg_api", "fg_binning", "fg_order", "fg_backward", "fg_oc_helper", "fg_query_group", "fg_query_small",
-                       "fg_index_sort", "fg_rows")]
+                       "fg_index_sort", "fg_rows", "fg_row_sums")]
     for d in QUERY_DIMS:
         out.append((os.path.join(CSRC, "fg_query_inst.hip"), os.path.join(OBJ, "fg_query_d%d.o" % d),
                     ["-DFG_QUERY_D=%d" % d] + (["-falign-loops=64"] if d in ALIGNED_DIMS else [])))

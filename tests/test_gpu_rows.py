@@ -210,6 +210,22 @@ def test_one_row_named_by_many():
     R.check(got, ref, mass, count[:, None], torch.float32)
 
 
+def test_a_row_of_five_million_entries():
+    """Enough for larger chunks: those of a row are added up by one lane"""
+    rng = np.random.default_rng(11)
+    m = 5_000_011
+    index = np.full(m, 1, dtype=np.int32)
+    index[:70] = 0
+    index[-5:] = -1
+    grad = values(rng, m, 4, torch.float16)
+    got = B.fg_lookup_backward(grad, B.fg_index_sort(dev(index), 3), dtype=torch.float32)
+    wide = R.wide(grad)
+    ref = np.stack([wide[:70].sum(0), wide[70:-5].sum(0), np.zeros(4)])
+    mass = np.stack([abs(wide[:70]).sum(0), abs(wide[70:-5]).sum(0), np.zeros(4)])
+    # no sum here is longer than some 5000 terms in a row (a chunk, the chunks of one, those): far fewer roundings than entries
+    R.check(got, ref, mass, 5000, torch.float32)
+
+
 def test_what_is_not_finite_stays_in_its_row():
     rng = np.random.default_rng(6)
     index = some_index(rng, (400,), 20)
@@ -401,6 +417,52 @@ def test_on_a_stream_of_its_own():
     sent2 = B.fg_dispatch(x, by.place, torch.zeros((2000, 320), dtype=torch.bfloat16, device=DEV))
     assert torch.equal(sent, sent2) and torch.equal(out, B.fg_combine(sent2, by.place, w))
     assert all(torch.equal(a, b) for a, b in zip(grads, B.fg_combine_backward(x, sent2, by.place, w)))
+
+
+@pytest.mark.parametrize("m,n_rows", [(1_200_000, 1_000_000), (300_000, 77)])
+def test_a_large_sort_captured_and_replayed(m, n_rows):
+    rng = np.random.default_rng(m)
+    index = torch.zeros(m, dtype=torch.int32, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        B.fg_index_sort(index, n_rows)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = B.fg_index_sort(index, n_rows)
+    for seed in range(4):
+        index.copy_(dev(some_index(rng, (m,), n_rows, "frequent" if seed % 2 else "uniform")))
+        graph.replay()
+        torch.cuda.synchronize()
+        now = B.fg_index_sort(index, n_rows)
+        assert torch.equal(got.order, now.order) and torch.equal(got.bounds, now.bounds) and torch.equal(got.place, now.place)
+        torch.cuda.synchronize()
+
+
+def test_two_at_once():
+    """The same calls on two streams, with what the allocator gives each, over and over: no result depends on the other's"""
+    rng = np.random.default_rng(31)
+    n, t, k, c = 3000, 20000, 6, 64
+    sets = [(dev(some_index(rng, (t, k), n, "frequent")), values(rng, n, c, torch.float32), values(rng, t, c, torch.float32),
+             dev(rng.random((t, k)).astype(np.float32))) for _ in range(2)]
+
+    def step(index, rows, grad, w):
+        by = B.fg_index_sort(index, n)
+        return (B.fg_combine(rows, index, w), *B.fg_combine_backward(grad, rows, index, w, sort=by), by.order)
+    alone = [step(*s) for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    got = [[], []]
+    for _ in range(5):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(step(*sets[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for again in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(alone[i], again))
 
 
 @pytest.mark.parametrize("t", [70, 5000])
