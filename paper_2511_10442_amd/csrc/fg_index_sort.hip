@@ -4,20 +4,28 @@
 // sums over them come out the same in every run.  An entry outside 0..n_rows-1 has the key n_rows, behind all rows.  A pass of a tile:
 // 64 entries at a time a wavefront finds, with one ballot for every bit of the digit, which lanes have the same digit; the number of
 // those before a lane is its rank, their count moves the wavefront's counter of that digit.
+//
+// Up to 8192 entries one workgroup sorts in LDS, all digits in one launch: 256 entries of 128 rows 4.1 us, 1000 of 5003 6.6.  Beyond, three launches a
+// digit (counts of the tiles, their prefix, the entries to their places) and one for the bounds: 262144 entries of 64 rows 15 us, 65536 of 131072 30
+// (latency: a tile's chain of loads, ranks and stores is 5 to 7 us, however few there are), 4M of 100k 82, 32M of 1M 720.  A pass over 4M moves 48 to 64 MB
+// in 23 to 26 us: stores of runs of 8 entries.
 #include "fg_rows.hpp"
 
 namespace fg {
 
 namespace {
 
-constexpr int kMaxBits = 10;                 // of a digit: counters of a wavefront stay below 4 KiB of LDS
+constexpr int kMaxBits = 10;                 // of a digit: a million rows in two passes
 constexpr int kSmallBlock = 1024;
-constexpr int64_t kSmallM = 8192;            // entries that one workgroup sorts in LDS
-constexpr int64_t kSmallRows = 1024;         // rows whose bounds a workgroup writes: for more, more workgroups sort the same entries
+constexpr int64_t kSmallM = 8192;            // entries that one workgroup sorts in LDS (8192 of 50000 rows 18 us, with the launches for more 27)
+// Rows whose bounds a workgroup writes; for more, more workgroups sort the same entries (1000 entries of 5003 rows: one workgroup and a search of the
+// bounds in a launch of its own 8.8 us, five 6.6).
+constexpr int64_t kSmallRows = 1024, kSmallBlocks = 256;
 constexpr int kBlock = 256;
 constexpr unsigned kXcds = 8;
-constexpr int64_t kSmallBlocks = 256;
-constexpr int kItems = 4;                    // a tile: kBlock x kItems entries, or beyond kMediumM
+// A tile: few entries, so that there are many, up to a million; then runs that are worth storing (4M entries of 100k rows, us, by threads x entries
+// of a tile: 256 x 8 101, 256 x 16 108, 512 x 4 96, 512 x 8 84, 512 x 16 101, 1024 x 4 90, 1024 x 8 92).
+constexpr int kItems = 4;
 constexpr int64_t kMediumM = 1 << 20;
 constexpr int kLargeBlock = 512, kLargeItems = 8;
 
@@ -262,7 +270,8 @@ __global__ __launch_bounds__(kBlock) void k_sort_scan(uint32_t* __restrict__ cou
     if (threadIdx.x == 0) totals[blockIdx.x] = before;
 }
 
-// A tile is put in order in LDS first, so that its entries of one digit leave as one run; runs of neighbouring tiles lie next to each other.
+// A tile is put in order in LDS first, so that its entries of one digit leave as one run; runs of neighbouring tiles lie next to each other.  (4M
+// entries: every lane storing its own 75 us a pass, runs 38, with more wavefronts a workgroup 25.)
 // FIRST: keys are the index itself and entries are numbered as they come.  LAST: place is written, with one pass in all the bounds too.
 template <int BLOCK, int ITEMS>
 constexpr size_t scatter_lds(int digits) { return ((size_t)digits * (BLOCK / 64 + 1) + 2 * BLOCK * ITEMS) * 4; }
@@ -424,6 +433,7 @@ hipError_t launch_index_sort(const int32_t* index, int64_t m, int64_t n_rows, in
     if (takes_small_sort(m)) {
         if (m <= kSmallBlock) return small<1>(index, m, n_rows, p, order, place, bounds, stream);
         if (m <= 2 * kSmallBlock) return small<2>(index, m, n_rows, p, order, place, bounds, stream);
+        if (m <= 4 * kSmallBlock) return small<4>(index, m, n_rows, p, order, place, bounds, stream);
         return small<8>(index, m, n_rows, p, order, place, bounds, stream);
     }
     if (!p.large) return many<kBlock, kItems>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);

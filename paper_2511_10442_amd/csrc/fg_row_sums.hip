@@ -9,10 +9,11 @@ namespace {
 // ---- sums over the entries of a row ------------------------------------------------------------------------------------
 
 // Rows that are named often are summed in parts: `chunk` entries of the sorted index that all name one row, and kChunks such chunks, are summed
-// by themselves and put together afterwards, so that what one lane does for a row hardly grows with the row's entries.  chunk is kChunk, or where
-// rows alone make 512 wavefronts, four times the mean of a row's entries (a power of two): rows of a graph are named often, but all of them, and as
-// chunks they would be read by a few scattered lanes (20k points, 40 neighbours of 64 float32, us: 57 with chunks of 32, 42 so; 100k entries of 1000 rows of
-// 512 bf16 28 and 22).
+// by themselves and put together afterwards, so that what one lane does for a row hardly grows with the row's entries.  chunk is kChunk,
+// or, for rows of a graph are named often, but all of them, and as chunks they would be read by a few scattered lanes, four times the mean of a row's
+// entries, as far as the rows alone give 512 lanes for every entry of a chunk, so that one lane's share stays small beside the whole (a power of two;
+// 20k points, 40 neighbours of 64 float32: 57 us with chunks of 32, 42 with 256; 9k points, 100 neighbours of 128 78 and 50; but entries whose rows follow
+// Zipf's law, 1M of 5000 rows of 64 bf16, 308 us with 64 lanes, 90 with 256, 62 so; 66k of 105 rows of 2112 147, 90, 80).
 //   k_row_sums   chunks of one row each, a row's first and last with its entries before and after them: their sums; rows without such a chunk
 //   k_row_parts  chunks of chunks (where there are enough entries)
 //   k_row_join   rows with a chunk: chunks up to the first whole chunk of chunks, those, and chunks again
@@ -310,7 +311,7 @@ hipError_t row_sums(const RowSums& r, const SumArgs& a, hipStream_t stream)
     int64_t chunk = kChunk;
     b.shift = 5;
     // (and with very many entries: chunks of chunks that one lane may have to add up stay below 4096)
-    while (chunk < 65536 && ((r.n_rows * pieces >= kFill / 16 && chunk < 4 * (r.m / r.n_rows)) || r.m / (chunk * kChunks) > 4096)) { chunk *= 2; ++b.shift; }
+    while (chunk < 65536 && ((chunk < 4 * (r.m / r.n_rows) && 2 * chunk * 512 <= r.n_rows * pieces) || r.m / (chunk * kChunks) > 4096)) { chunk *= 2; ++b.shift; }
     b.chunks = r.m / chunk;
     b.parts = r.partials;
     b.parts2 = nullptr;

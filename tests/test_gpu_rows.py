@@ -47,8 +47,8 @@ def check_sort(index, n_rows, **kw):
         assert got.place is None
 
 
-# one workgroup with 1, 2 and 8 entries a lane, many workgroups with 4 and 16; bounds from one workgroup, from the digits, by search
-@pytest.mark.parametrize("m", [0, 1, 63, 64, 65, 1024, 1025, 2048, 2049, 8192, 8193, 20011])
+# one workgroup with 1, 2, 4 and 8 entries a lane, many workgroups with 4 and 16; bounds from one workgroup, from the digits, by search
+@pytest.mark.parametrize("m", [0, 1, 63, 64, 65, 1024, 1025, 2048, 2049, 4096, 4097, 8192, 8193, 20011])
 @pytest.mark.parametrize("n_rows", [0, 1, 2, 7, 64, 1000, 1023, 1024, 4096, 4097, 70001])
 def test_sort(m, n_rows):
     rng = np.random.default_rng(m * 31 + n_rows)
