@@ -310,9 +310,13 @@ fg_status fg_dispatch(const void* x, int32_t type, int64_t t, int64_t c, int64_t
 /* out[i] = sum over j of weights[i][j] * rows[index[i][j]]: experts' answers back to their tokens (index = place), or the
  * message that a point receives from its neighbours (index = fg_binned_select_knn's out_idx).
  *   rows [n_rows][c], index [t][k], weights [t][k] or NULL (all 1), out [t][c] of the rows' type.
- * Entries that name no row add nothing, whatever their weight. */
+ * Entries that name no row add nothing, whatever their weight.
+ *   walk [t] or NULL: the order in which the rows of out are made, a permutation of 0..t-1 (with anything else it is not specified
+ *              which rows are written).  It changes no result, only the speed: where rows are shared, those that share them should
+ *              follow each other.  For a graph of points in no order, fg_bin_points' order of them (Binning.perm, the index fields of
+ *              sorted_points) halves the time. */
 fg_status fg_combine(const void* rows, int32_t type, int64_t n_rows, int64_t c, int64_t rows_stride, const int32_t* index,
-                     const float* weights, int64_t t, int32_t k, void* out, int64_t out_stride, void* stream);
+                     const float* weights, int64_t t, int32_t k, const int32_t* walk, void* out, int64_t out_stride, void* stream);
 
 /* Gradients of fg_combine:
  *   grad_rows[v]       = sum over the entries (i, j) that name v of weights[i][j] * grad_out[i]
@@ -322,12 +326,13 @@ fg_status fg_combine(const void* rows, int32_t type, int64_t n_rows, int64_t c, 
  * order, bounds: both NULL: no row is named twice (index = place); rows that no entry names are left as they were, and a row that
  * is named twice gets one of its terms.  Both given (fg_index_sort of index [t*k]): rows may be named any number of times, and
  * all of grad_rows is written.
+ *   walk [n_rows] or NULL: with them, the order in which the rows of grad_rows are made, as for fg_combine; else without effect.
  * workspace (with order and grad_rows only): fg_combine_backward_workspace_size() bytes, 256-byte aligned; NULL where that is 0. */
 fg_status fg_combine_backward_workspace_size(int64_t t, int32_t k, int64_t c, int32_t type, size_t* bytes /* host out */);
 fg_status fg_combine_backward(const void* grad_out, int32_t type, int64_t t, int64_t c, int64_t grad_stride, const void* rows,
                               int64_t n_rows, int64_t rows_stride, const int32_t* index, const float* weights, int32_t k,
-                              const int32_t* order, const int32_t* bounds, void* grad_rows, int64_t grad_rows_stride,
-                              float* grad_weights, void* workspace, size_t workspace_bytes, void* stream);
+                              const int32_t* order, const int32_t* bounds, const int32_t* walk, void* grad_rows,
+                              int64_t grad_rows_stride, float* grad_weights, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -97,9 +97,9 @@ def lib() -> ctypes.CDLL:
                 "fg_lookup_backward_workspace_size": [i64, i64, i32, psz],
                 "fg_lookup_backward": [vp, i32, i64, i64, i64, vp, vp, vp, i64, f32, i32, vp, i32, i64, vp, sz, vp],
                 "fg_dispatch": [vp, i32, i64, i64, i64, vp, i32, i64, vp, i64, vp],
-                "fg_combine": [vp, i32, i64, i64, i64, vp, vp, i64, i32, vp, i64, vp],
+                "fg_combine": [vp, i32, i64, i64, i64, vp, vp, i64, i32, vp, vp, i64, vp],
                 "fg_combine_backward_workspace_size": [i64, i32, i64, i32, psz],
-                "fg_combine_backward": [vp, i32, i64, i64, i64, vp, i64, i64, vp, vp, i32, vp, vp, vp, i64, vp, vp, sz, vp]}.items():
+                "fg_combine_backward": [vp, i32, i64, i64, i64, vp, i64, i64, vp, vp, i32, vp, vp, vp, vp, i64, vp, vp, sz, vp]}.items():
             fn = getattr(L, name)
             fn.restype, fn.argtypes = ctypes.c_int, args
         _lib = L
@@ -596,8 +596,18 @@ def fg_dispatch(x: torch.Tensor, place: torch.Tensor, out: torch.Tensor | None =
     return out
 
 
-def fg_combine(rows: torch.Tensor, index: torch.Tensor, weights: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
-    """out[i] = sum_j weights[i, j] * rows[index[i, j]]: [t, c] of the rows' dtype."""
+def _walk(t, n: int, device):
+    if t is None:
+        return None
+    if t.shape != (n,):
+        raise ValueError("walk must have shape (%d,)" % n)
+    return _index(t, "walk", device)
+
+
+def fg_combine(rows: torch.Tensor, index: torch.Tensor, weights: torch.Tensor | None = None, out: torch.Tensor | None = None,
+               walk: torch.Tensor | None = None) -> torch.Tensor:
+    """out[i] = sum_j weights[i, j] * rows[index[i, j]]: [t, c] of the rows' dtype.  walk [t]: the order in which they are made, a permutation
+    (for a graph, Binning.perm: several times as fast where the points are in no order)."""
     dev = rows.device
     at, stride = _row_view(rows, "rows")
     names = _index(index, "index", dev, 2)
@@ -609,15 +619,15 @@ def fg_combine(rows: torch.Tensor, index: torch.Tensor, weights: torch.Tensor | 
         to, to_stride = out.data_ptr() or None, c
     else:
         to, to_stride = _row_view(out, "out", rows.dtype, dev, (t, c))
-    _call("fg_combine", dev, at, _TYPES[rows.dtype], n, c, stride, names, w, t, k, to, to_stride)
+    _call("fg_combine", dev, at, _TYPES[rows.dtype], n, c, stride, names, w, t, k, None if walk is None else _walk(walk, t, dev), to, to_stride)
     return out
 
 
 def fg_combine_backward(grad_out: torch.Tensor, rows: torch.Tensor, index: torch.Tensor, weights: torch.Tensor | None = None,
                         sort: IndexSort | None = None, grad_rows: torch.Tensor | None = None, grad_weights: torch.Tensor | None = None,
-                        workspace: torch.Tensor | None = None):
+                        workspace: torch.Tensor | None = None, walk: torch.Tensor | None = None):
     """(gradient of rows, gradient of weights or None where there are none).  sort: fg_index_sort(index, len(rows)), needed where entries
-    share rows; without it every row is named once at most, and rows that none names keep what grad_rows has (zeros if it is not given)."""
+    share rows (walk [len(rows)]: the order in which they are taken, as for fg_combine); without it every row is named once at most, and rows that none names keep what grad_rows has (zeros if it is not given)."""
     dev = rows.device
     n, c = rows.shape
     at, stride = _row_view(rows, "rows")
@@ -639,6 +649,7 @@ def fg_combine_backward(grad_out: torch.Tensor, rows: torch.Tensor, index: torch
         grad_weights = torch.empty((t, k), dtype=torch.float32, device=dev)
     gw = _weights(grad_weights, index.shape, dev, "grad_weights")
     ws = _scratch(workspace, size, dev)
-    _call("fg_combine_backward", dev, grad, _TYPES[rows.dtype], t, c, grad_stride, at, n, stride, names, w, k, order, bounds, to, to_stride, gw,
+    _call("fg_combine_backward", dev, grad, _TYPES[rows.dtype], t, c, grad_stride, at, n, stride, names, w, k, order, bounds,
+          None if walk is None else _walk(walk, n, dev), to, to_stride, gw,
           _ptr(ws), _bytes(ws))
     return grad_rows, grad_weights

@@ -617,7 +617,7 @@ fg_status fg_dispatch(const void* x, int32_t type, int64_t t, int64_t c, int64_t
 }
 
 fg_status fg_combine(const void* rows, int32_t type, int64_t n_rows, int64_t c, int64_t rows_stride, const int32_t* index,
-                     const float* weights, int64_t t, int32_t k, void* out, int64_t out_stride, void* stream)
+                     const float* weights, int64_t t, int32_t k, const int32_t* walk, void* out, int64_t out_stride, void* stream)
 {
     const fg_status st = check_rows(type, c, {rows_stride}, {out_stride});
     if (st != FG_OK) return st;
@@ -625,7 +625,7 @@ fg_status fg_combine(const void* rows, int32_t type, int64_t n_rows, int64_t c, 
     if (t == 0) return FG_OK;
     if (!index || !out || (!rows && n_rows > 0)) return FG_ERR_NULL;
     if (misaligned(type, {rows, out})) return FG_ERR_UNSUPPORTED;
-    return told(launch_combine(type, {rows, rows_stride}, n_rows, c, index, weights, t, k, {out, out_stride}, (hipStream_t)stream));
+    return told(launch_combine(type, {rows, rows_stride}, n_rows, c, index, weights, t, k, walk, {out, out_stride}, (hipStream_t)stream));
 }
 
 fg_status fg_combine_backward_workspace_size(int64_t t, int32_t k, int64_t c, int32_t type, size_t* bytes)
@@ -640,8 +640,8 @@ fg_status fg_combine_backward_workspace_size(int64_t t, int32_t k, int64_t c, in
 
 fg_status fg_combine_backward(const void* grad_out, int32_t type, int64_t t, int64_t c, int64_t grad_stride, const void* rows,
                               int64_t n_rows, int64_t rows_stride, const int32_t* index, const float* weights, int32_t k,
-                              const int32_t* order, const int32_t* bounds, void* grad_rows, int64_t grad_rows_stride,
-                              float* grad_weights, void* workspace, size_t workspace_bytes, void* stream)
+                              const int32_t* order, const int32_t* bounds, const int32_t* walk, void* grad_rows,
+                              int64_t grad_rows_stride, float* grad_weights, void* workspace, size_t workspace_bytes, void* stream)
 {
     fg_status st = check_rows(type, c, {grad_stride});
     if (st == FG_OK && grad_weights) st = check_rows(type, c, {rows_stride});
@@ -659,7 +659,7 @@ fg_status fg_combine_backward(const void* grad_out, int32_t type, int64_t t, int
         RowSums a = {};
         a.type = type; a.out_type = type;
         a.grad = {grad_out, grad_stride}; a.out = {grad_rows, grad_rows_stride};
-        a.index = index; a.order = order; a.bounds = bounds; a.weights = weights;
+        a.index = index; a.order = order; a.bounds = bounds; a.weights = weights; a.walk = walk;
         a.m = t * k; a.n_rows = n_rows; a.c = c; a.fan = k; a.scale = 1.0f;
         if (products) { a.rows = {rows, rows_stride}; a.grad_weights = grad_weights; }
         a.partials = (float*)workspace;

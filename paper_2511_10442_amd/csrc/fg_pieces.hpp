@@ -19,6 +19,8 @@ constexpr int64_t kFill = 256 * 2048;        // lanes that the chip holds at a t
 // Eight workgroups for every place on the chip; more work than that: they take several turns.  Where pieces differ in what they take, a workgroup that is
 // done makes room for the next instead (64k tokens' gradient, the commonest 4000 times: 313 us in turns, 300 so).
 constexpr int64_t kMostBlocks = 1 << 14, kMostUneven = 1 << 20;
+// Times that a row is named, on average, from which on rows are expected to be found in an XCD's L2 by those that name them too (kShared: by_xcd)
+constexpr int64_t kShared = 4;
 constexpr int64_t kFewWaves = 256 * 16;      // half of the wavefronts that the chip holds
 // Bytes that a call moves, twice the last-level cache, from which on most of its output has left that cache when the call ends: it is stored past the
 // caches (64k rows of 4 KiB looked up 75 -> 61 us; 32k sums of 8 rows of 4 KiB 236 -> 224, with the rows' loads 209; a gradient of 1 GiB 319 -> 297).
@@ -119,24 +121,32 @@ __device__ __forceinline__ Span<SEGS> span_of(const Deal& d, int64_t row, uint32
     }
     return at;
 }
-// SEGS == 0: one after the other
+// SEGS == 0: one after the other.  `block` of `blocks` has a share.
 template <int N, int SEGS, typename Body>
-__device__ __forceinline__ void each_span(const Deal& d, Body&& body)
+__device__ __forceinline__ void each_span(const Deal& d, int64_t block, int64_t blocks, Body&& body)
 {
     if constexpr (SEGS > 0) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-        for (int64_t unit = (int64_t)blockIdx.x * (kBlock / 64) + wave; unit < d.units; unit += (int64_t)gridDim.x * (kBlock / 64)) {
+        for (int64_t unit = block * (kBlock / 64) + wave; unit < d.units; unit += blocks * (kBlock / 64)) {
             const int64_t row = d.by_waves_far(unit);
             body(span_of<N, SEGS>(d, row, (uint32_t)(unit - row * d.waves) * (64 * SEGS) + lane));
         }
     } else {
-        for (int64_t first = (int64_t)blockIdx.x * kBlock; first < d.total; first += (int64_t)gridDim.x * kBlock) {
+        for (int64_t first = block * kBlock; first < d.total; first += blocks * kBlock) {
             const int64_t row0 = d.by_pieces_far(first);
             const uint32_t x = (uint32_t)(first - row0 * d.pieces) + threadIdx.x, q = d.by_pieces(x);
             if (first + threadIdx.x < d.total) body(span_of<N, 1>(d, row0 + q, x - q * d.pieces));
         }
     }
 }
+template <int N, int SEGS, typename Body>
+__device__ __forceinline__ void each_span(const Deal& d, Body&& body)
+{
+    each_span<N, SEGS>(d, (int64_t)blockIdx.x, (int64_t)gridDim.x, body);
+}
+// Workgroups go to the XCDs in turn; so counted, each XCD has one run of them, and rows that are near in the order meet in its L2.  blocks: a multiple of kXcds.
+constexpr int64_t kXcds = 8;
+__device__ __forceinline__ int64_t by_xcd(int64_t block, int64_t blocks) { return block % kXcds * (blocks / kXcds) + block / kXcds; }
 
 Deal deal(int64_t rows, int64_t c, uint32_t pieces, int most_segs)
 {
@@ -164,16 +174,17 @@ dim3 blocks_for(int64_t total, int64_t each, int64_t most = kMostBlocks)
     const int64_t b = (total + each - 1) / each;
     return dim3((unsigned)(b < most ? b : most));
 }
+unsigned to_xcds(dim3 grid) { return (unsigned)((grid.x + kXcds - 1) / kXcds * kXcds); }
 dim3 blocks_for(const Deal& d, int64_t most) { return d.segs ? blocks_for(d.units, kBlock / 64, most) : blocks_for(d.total, kBlock, most); }
 // A launch of a kernel by how its pieces are dealt out (SEGS, the kernel's last template argument: up to MOST); N == 1: rows of up to seven elements,
 // one after the other
-#define FG_LAUNCH_DEAL(MOST, d, most, stream, kernel, ...)                                                                     \
-    do {                                                                                                                       \
-        constexpr int fg_4 = N > 1 && MOST >= 4 ? 4 : 0, fg_2 = N > 1 && MOST >= 2 ? 2 : 0, fg_1 = N > 1 ? 1 : 0;              \
-        if (fg_4 && (d).segs == 4) FG_LAUNCH((kernel, fg_4>), blocks_for(d, most), dim3(kBlock), 0, stream, __VA_ARGS__);      \
-        else if (fg_2 && (d).segs == 2) FG_LAUNCH((kernel, fg_2>), blocks_for(d, most), dim3(kBlock), 0, stream, __VA_ARGS__); \
-        else if (fg_1 && (d).segs == 1) FG_LAUNCH((kernel, fg_1>), blocks_for(d, most), dim3(kBlock), 0, stream, __VA_ARGS__); \
-        else FG_LAUNCH((kernel, 0>), blocks_for((d).total, kBlock, most), dim3(kBlock), 0, stream, __VA_ARGS__);               \
+#define FG_LAUNCH_DEAL(MOST, d, grid, stream, kernel, ...)                                                              \
+    do {                                                                                                                \
+        constexpr int fg_4 = N > 1 && MOST >= 4 ? 4 : 0, fg_2 = N > 1 && MOST >= 2 ? 2 : 0, fg_1 = N > 1 ? 1 : 0;       \
+        if (fg_4 && (d).segs == 4) FG_LAUNCH((kernel, fg_4>), dim3(grid), dim3(kBlock), 0, stream, __VA_ARGS__);        \
+        else if (fg_2 && (d).segs == 2) FG_LAUNCH((kernel, fg_2>), dim3(grid), dim3(kBlock), 0, stream, __VA_ARGS__);   \
+        else if (fg_1 && (d).segs == 1) FG_LAUNCH((kernel, fg_1>), dim3(grid), dim3(kBlock), 0, stream, __VA_ARGS__);   \
+        else FG_LAUNCH((kernel, 0>), dim3(grid), dim3(kBlock), 0, stream, __VA_ARGS__);                                 \
     } while (0)
 
 // ---- entries, several at a time ----------------------------------------------------------------------------------------

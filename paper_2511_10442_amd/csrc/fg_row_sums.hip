@@ -23,7 +23,8 @@ namespace {
 // Bound by memory: the gradient of 131072 x 2048 float32 from 64k tokens in bf16, the commonest of which comes 4000 times, takes 245 us + 13 for the
 // long rows (1.33 GB at 5.2 TB/s); 131072 x 4096 bf16 from 20k tokens 157, what filling it with zeros takes.  In a graph of 100k points with
 // 40 neighbours each, 64 float32 a point, 235 us with the weights' gradient: 125 for the points' rows (1 GB out of the last-level cache), 60 for a
-// weight and 50 for its gradient an entry, 4 bytes each in a line of its own.  (The products in a kernel of their own: 170 + 150.)
+// weight and 50 for its gradient an entry, 4 bytes each in a line of its own.  (The products in a kernel of their own: 170 + 150.)  Taken in the order of
+// the points' bins (walk), 104.
 constexpr int kChunk = 32, kChunks = 32;
 constexpr int64_t kPartsFrom = 16;           // chunks of chunks from which on it is looked whether there are any
 
@@ -35,6 +36,7 @@ struct SumArgs {
     int64_t n_rows;
     int64_t chunks;          // m / chunk
     Divide by_fan;
+    const int32_t* walk;     // the order in which rows are taken, or NULL
     float scale;
     int32_t shift;           // log2 of chunk
     float *parts, *parts2;   // sums of chunks, and of chunks of chunks (NULL: none)
@@ -146,43 +148,58 @@ __device__ __forceinline__ void store_sum(const SumArgs& a, typename Piece<T, N>
     }
 }
 
+// The first chunk_blocks workgroups have the chunks (dc), the others the rows (d).
 template <typename T, int N, typename TO, bool WEIGHTED, bool ACCUMULATE, bool DOTS, bool STREAM, int SEGS>
-__global__ __launch_bounds__(kBlock, DOTS && sizeof(T) == 2 ? 3 : 4) void k_row_sums(SumArgs a, const int32_t* __restrict__ index, const int32_t* __restrict__ order,
-                                                                                     const int32_t* __restrict__ bounds, const float* __restrict__ weights,
-                                                                                     const T* __restrict__ grad, int64_t grad_stride,
-                                                                                     const T* __restrict__ rows, int64_t rows_stride,
-                                                                                     TO* __restrict__ out, int64_t out_stride, Deal d)
+__global__ __launch_bounds__(kBlock, DOTS && sizeof(T) == 2 ? 3 : 4) void k_row_sums(SumArgs a, const int32_t* __restrict__ index,
+                                                                                     const int32_t* __restrict__ order, const int32_t* __restrict__ bounds,
+                                                                                     const float* __restrict__ weights, const T* __restrict__ grad,
+                                                                                     int64_t grad_stride, const T* __restrict__ rows, int64_t rows_stride,
+                                                                                     TO* __restrict__ out, int64_t out_stride, Deal dc, Deal d,
+                                                                                     unsigned chunk_blocks, bool shared)
 {
     typedef Piece<T, N> P;
     constexpr int S = SEGS ? SEGS : 1;
     a.index = index; a.order = order; a.bounds = bounds; a.weights = weights;        // (arguments of their own: nothing stored changes them)
-    each_span<N, SEGS>(d, [&](const Span<S>& at) {
-        const bool real = !DOTS || at.skip[0] < N;
-        if (at.row < a.chunks) {
+    const bool chunk = blockIdx.x < chunk_blocks;
+    int64_t block = chunk ? blockIdx.x : blockIdx.x - chunk_blocks;
+    const int64_t blocks = chunk ? chunk_blocks : gridDim.x - chunk_blocks;
+    if (!chunk && shared) block = by_xcd(block, blocks);
+    const Deal& all = chunk ? dc : d;
+    each_span<N, SEGS>(all, block, blocks, [&](const Span<S>& at) {
+        int64_t name = at.row;
+        int32_t from, to;
+        if (chunk) {
             const int32_t q = (int32_t)at.row;
-            int32_t name;
-            if (!one_row(a, q << a.shift, 1 << a.shift, name)) return;
-            int32_t from = a.bounds[name], to = a.bounds[name + 1];
+            int32_t of;
+            if (!one_row(a, q << a.shift, 1 << a.shift, of)) return;
+            name = of;
+            from = a.bounds[name];
+            to = a.bounds[name + 1];
             within(a, from, to);
             if (first_chunk(a, from) < q) from = q << a.shift;
             if (to >> a.shift > q + 1) to = (q + 1) << a.shift;
-            typename P::Wide sum[S] = {}, row = {};
-            if (DOTS) row = wide<T, N>(load_piece<T, N>(rows + (int64_t)name * rows_stride + at.col[0]));
-            add_entries<T, N, WEIGHTED, DOTS, S>(sum, a, grad, grad_stride, from, to, at, row, real, (int)d.pieces);
-#pragma unroll
-            for (int s = 0; s < S; ++s)
-                if (real && at.there[s]) *reinterpret_cast<typename P::Wide*>(a.parts + (at.row * d.pieces + at.piece[s]) * N) = sum[s];
-            return;
+        } else {
+            if (a.walk) {
+                name = (uint32_t)a.walk[name];
+                if (name >= a.n_rows) return;
+            }
+            from = a.bounds[name];
+            to = a.bounds[name + 1];
+            within(a, from, to);
+            if (first_chunk(a, from) < to >> a.shift) return;              // k_row_join
+            if (ACCUMULATE && from >= to) return;
         }
-        const int64_t name = at.row - a.chunks;
-        int32_t from = a.bounds[name], to = a.bounds[name + 1];
-        within(a, from, to);
-        if (first_chunk(a, from) < to >> a.shift) return;                  // k_row_join
-        if (ACCUMULATE && from >= to) return;
+        const bool real = !DOTS || at.skip[0] < N;
         typename P::Wide sum[S] = {}, row = {};
         if (DOTS && from < to) row = wide<T, N>(load_piece<T, N>(rows + name * rows_stride + at.col[0]));
         add_entries<T, N, WEIGHTED, DOTS, S>(sum, a, grad, grad_stride, from, to, at, row, real, (int)d.pieces);
-        store_sum<T, N, TO, ACCUMULATE, STREAM, S>(a, sum, out, out_stride, name, at);
+        if (chunk) {
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+                if (real && at.there[s]) *reinterpret_cast<typename P::Wide*>(a.parts + (at.row * d.pieces + at.piece[s]) * N) = sum[s];
+        } else {
+            store_sum<T, N, TO, ACCUMULATE, STREAM, S>(a, sum, out, out_stride, name, at);
+        }
     });
 }
 
@@ -315,13 +332,24 @@ hipError_t row_sums(const RowSums& r, const SumArgs& a, hipStream_t stream)
     b.chunks = r.m / chunk;
     b.parts = r.partials;
     b.parts2 = nullptr;
-    const Deal d = deal(b.chunks + r.n_rows, r.c, pieces, DOTS ? 1 : 2);
+    const Deal d = deal(r.n_rows, r.c, pieces, DOTS ? 1 : 2);
+    Deal dc = deal(b.chunks, r.c, pieces, d.segs);
+    if (dc.segs != d.segs) {                                 // few chunks: the same kernel's all the same
+        dc.segs = d.segs;
+        dc.waves = d.waves;
+        dc.by_waves_far = d.by_waves_far;
+        dc.units = b.chunks * dc.waves;
+    }
+    const bool shared = r.fan > 1 && r.m >= kShared * r.n_rows;       // (fan == 1: no row of grad is read twice)
+    const unsigned chunk_blocks = b.chunks ? to_xcds(blocks_for(dc, kMostUneven)) : 0, row_blocks = to_xcds(blocks_for(d, kMostUneven));
 #define FG_SUMS(STREAM) k_row_sums<T, N, TO, WEIGHTED, ACCUMULATE, DOTS, STREAM
-#define FG_SUMS_ARGS b, b.index, b.order, b.bounds, b.weights, grad, r.grad.stride, rows, r.rows.stride, (TO*)r.out.at, r.out.stride, d
+#define FG_SUMS_ARGS                                                                                                                     \
+    b, b.index, b.order, b.bounds, b.weights, grad, r.grad.stride, rows, r.rows.stride, (TO*)r.out.at, r.out.stride, dc, d, chunk_blocks, shared
     const bool past = !ACCUMULATE && !DOTS && (r.n_rows * (int64_t)sizeof(TO) + r.m / r.fan * (int64_t)sizeof(T)) * r.c >= kStream;
-    if constexpr (DOTS) FG_LAUNCH_DEAL(1, d, kMostUneven, stream, FG_SUMS(false), FG_SUMS_ARGS);
-    else if (!past) FG_LAUNCH_DEAL(2, d, kMostUneven, stream, FG_SUMS(false), FG_SUMS_ARGS);
-    else FG_LAUNCH_DEAL(2, d, kMostUneven, stream, FG_SUMS(!ACCUMULATE), FG_SUMS_ARGS);
+    const unsigned grid = chunk_blocks + row_blocks;
+    if constexpr (DOTS) FG_LAUNCH_DEAL(1, d, grid, stream, FG_SUMS(false), FG_SUMS_ARGS);
+    else if (!past) FG_LAUNCH_DEAL(2, d, grid, stream, FG_SUMS(false), FG_SUMS_ARGS);
+    else FG_LAUNCH_DEAL(2, d, grid, stream, FG_SUMS(!ACCUMULATE), FG_SUMS_ARGS);
 #undef FG_SUMS_ARGS
 #undef FG_SUMS
     if (!b.chunks && !DOTS) return hipSuccess;
@@ -372,7 +400,7 @@ bool sums_with_products(int32_t type, int64_t c)
 hipError_t launch_row_sums(const RowSums& r, hipStream_t stream)
 {
     SumArgs a = {};
-    a.index = r.index; a.order = r.order; a.bounds = r.bounds; a.weights = r.weights; a.grad_weights = r.grad_weights;
+    a.index = r.index; a.order = r.order; a.bounds = r.bounds; a.weights = r.weights; a.grad_weights = r.grad_weights; a.walk = r.walk;
     a.m = (int32_t)r.m; a.n_rows = r.n_rows; a.by_fan = Divide((uint32_t)r.fan); a.scale = r.scale;
     if (r.out_type == FG_F32 && r.type != FG_F32) {
         // pieces of 16 bytes of the output, most of what moves where a table is large

@@ -62,17 +62,26 @@ __global__ __launch_bounds__(kBlock) void k_dispatch(const T* __restrict__ x, in
 
 // out[i] = sum over j of weights[i][j] rows[index[i][j]], eight rows' pieces under way at a time.  Where every row is named once, 32k sums of 8 rows of
 // 4 KiB take 207 us (1.2 GB at 5.8 TB/s); messages along a graph, 200k points of 64 float32 with 40 neighbours each in no order, 282 us: 2 GB of
-// rows leave the last-level cache at 7.3 TB/s (110 us where neighbours are near in memory too).
+// rows leave the last-level cache at 7.3 TB/s.  `walk` is the order in which the sums are made: points of a neighbourhood one after the other, on one XCD
+// (shared), find each other's neighbours in its L2.  200k points in three dimensions, 40 nearest neighbours: 294 us in no order, 103 in that of their
+// bins (100k: 137 and 52; 1M, 32 neighbours: 1234 and 541).
 // (n_rows > 0: an entry that names no row reads row 0 and adds zeros in its place, so that no load waits behind a branch)
 template <typename T, int N, bool WEIGHTED, bool STREAM, int SEGS>
 __global__ __launch_bounds__(kBlock) void k_combine(const T* __restrict__ rows, int64_t rows_stride, uint32_t n_rows, const int32_t* __restrict__ index,
-                                                    const float* __restrict__ weights, int32_t k, T* __restrict__ out, int64_t out_stride, Deal d)
+                                                    const float* __restrict__ weights, int32_t k, const int32_t* __restrict__ walk, int64_t t, T* __restrict__ out,
+                                                    int64_t out_stride, Deal d, bool shared)
 {
     typedef Piece<T, N> P;
     constexpr int S = SEGS ? SEGS : 1;
-    each_span<N, SEGS>(d, [&](const Span<S>& at) {
+    const int64_t block = shared ? by_xcd(blockIdx.x, gridDim.x) : blockIdx.x;
+    each_span<N, SEGS>(d, block, gridDim.x, [&](const Span<S>& at) {
+        int64_t row = at.row;
+        if (walk) {
+            row = (uint32_t)walk[row];
+            if (row >= t) return;
+        }
         typename P::Wide sum[S] = {};
-        const int64_t base = at.row * k;
+        const int64_t base = row * k;
         in_chunks<8>(k, [&](auto count, int32_t j, int there) {
             constexpr int U = count.value;
             int32_t name[U];
@@ -99,7 +108,7 @@ __global__ __launch_bounds__(kBlock) void k_combine(const T* __restrict__ rows, 
         });
 #pragma unroll
         for (int s = 0; s < S; ++s)
-            if (at.there[s]) store_piece<T, N, STREAM>(out + at.row * out_stride + at.col[s], narrow<T, N>(sum[s]));
+            if (at.there[s]) store_piece<T, N, STREAM>(out + row * out_stride + at.col[s], narrow<T, N>(sum[s]));
     });
 }
 
@@ -188,7 +197,7 @@ hipError_t lookup(RowsIn table, int64_t n_rows, int64_t c, const int32_t* index,
 {
     const Deal d = deal<T, N>(m, c, 2);
 #define FG_LOOKUP(STREAM) \
-    FG_LAUNCH_DEAL(2, d, kMostBlocks, stream, FG_LOOKUP_OF(STREAM), (const T*)table.at, table.stride, (uint32_t)n_rows, index, scale, (T*)out.at, out.stride, d)
+    FG_LAUNCH_DEAL(2, d, blocks_for(d, kMostBlocks), stream, FG_LOOKUP_OF(STREAM), (const T*)table.at, table.stride, (uint32_t)n_rows, index, scale, (T*)out.at, out.stride, d)
 #define FG_LOOKUP_OF(STREAM) k_lookup<T, N, STREAM
     if (2 * m * c * (int64_t)sizeof(T) < kStream) FG_LOOKUP(false); else FG_LOOKUP(true);
 #undef FG_LOOKUP_OF
@@ -201,19 +210,22 @@ hipError_t dispatch(RowsIn x, int64_t t, int64_t c, const int32_t* place, int32_
 {
     const Deal d = deal<T, N>(t, c, 4);
 #define FG_DISPATCH k_dispatch<T, N
-    FG_LAUNCH_DEAL(4, d, kMostBlocks, stream, FG_DISPATCH, (const T*)x.at, x.stride, place, k, (uint32_t)n_rows, (T*)out.at, out.stride, d);
+    FG_LAUNCH_DEAL(4, d, blocks_for(d, kMostBlocks), stream, FG_DISPATCH, (const T*)x.at, x.stride, place, k, (uint32_t)n_rows, (T*)out.at, out.stride, d);
 #undef FG_DISPATCH
     return hipSuccess;
 }
 
 template <typename T, int N>
-hipError_t combine(RowsIn rows, int64_t n_rows, int64_t c, const int32_t* index, const float* weights, int64_t t, int32_t k, RowsOut out,
-                   hipStream_t stream)
+hipError_t combine(RowsIn rows, int64_t n_rows, int64_t c, const int32_t* index, const float* weights, int64_t t, int32_t k, const int32_t* walk,
+                   RowsOut out, hipStream_t stream)
 {
     if (n_rows == 0) return lookup<T, N>(rows, 0, c, index, t, 1.0f, out, stream);       // zeros
     const Deal d = deal<T, N>(t, c, 2);
-#define FG_COMBINE(WEIGHTED, STREAM) \
-    FG_LAUNCH_DEAL(2, d, kMostBlocks, stream, FG_COMBINE_OF(WEIGHTED, STREAM), (const T*)rows.at, rows.stride, (uint32_t)n_rows, index, weights, k, (T*)out.at, out.stride, d)
+    const bool shared = t * k >= kShared * n_rows;
+    const unsigned grid = shared ? to_xcds(blocks_for(d, kMostUneven)) : blocks_for(d, kMostBlocks).x;
+#define FG_COMBINE(WEIGHTED, STREAM)                                                                                                        \
+    FG_LAUNCH_DEAL(2, d, grid, stream, FG_COMBINE_OF(WEIGHTED, STREAM), (const T*)rows.at, rows.stride, (uint32_t)n_rows, index, weights, k, \
+                   walk, t, (T*)out.at, out.stride, d, shared)
 #define FG_COMBINE_OF(WEIGHTED, STREAM) k_combine<T, N, WEIGHTED, STREAM
     const bool past = n_rows >= t * k && (t * k + t) * c * (int64_t)sizeof(T) >= kStream;      // (rows that are named again are worth keeping)
     if (weights) { if (past) FG_COMBINE(true, true); else FG_COMBINE(true, false); }
@@ -271,9 +283,9 @@ hipError_t launch_dispatch(int32_t type, RowsIn x, int64_t t, int64_t c, const i
 }
 
 hipError_t launch_combine(int32_t type, RowsIn rows, int64_t n_rows, int64_t c, const int32_t* index, const float* weights, int64_t t, int32_t k,
-                          RowsOut out, hipStream_t stream)
+                          const int32_t* walk, RowsOut out, hipStream_t stream)
 {
-    FG_BY_TYPE(type, c, (combine<T, N>(rows, n_rows, c, index, weights, t, k, out, stream)))
+    FG_BY_TYPE(type, c, (combine<T, N>(rows, n_rows, c, index, weights, t, k, walk, out, stream)))
 }
 
 hipError_t launch_combine_grad(int32_t type, RowsIn grad_out, int64_t t, int64_t c, RowsIn rows, int64_t n_rows, const int32_t* index,

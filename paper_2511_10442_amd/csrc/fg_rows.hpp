@@ -32,7 +32,7 @@ hipError_t launch_lookup(int32_t type, RowsIn table, int64_t n_rows, int64_t c, 
 hipError_t launch_dispatch(int32_t type, RowsIn x, int64_t t, int64_t c, const int32_t* place, int32_t k, int64_t n_rows, RowsOut out,
                            hipStream_t stream);
 hipError_t launch_combine(int32_t type, RowsIn rows, int64_t n_rows, int64_t c, const int32_t* index, const float* weights, int64_t t, int32_t k,
-                          RowsOut out, hipStream_t stream);
+                          const int32_t* walk /* or NULL */, RowsOut out, hipStream_t stream);
 
 // grad_weights, and with grad_rows.at (every row named once at most) the rows' gradient too
 hipError_t launch_combine_grad(int32_t type, RowsIn grad_out, int64_t t, int64_t c, RowsIn rows, int64_t n_rows, const int32_t* index,
@@ -45,6 +45,7 @@ struct RowSums {
     RowsOut out;
     const int32_t *index, *order, *bounds;
     const float* weights;
+    const int32_t* walk;     // the order in which rows are taken, or NULL
     RowsIn rows;             // with grad_weights (sums_with_products): the rows that the entries name
     float* grad_weights;     // or NULL
     int64_t m, n_rows, c;

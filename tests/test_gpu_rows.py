@@ -341,6 +341,31 @@ def test_shared_rows(n, t, k, c, dtype):
     R.check(B.fg_combine(rows, dev(index), w), ref, mass, k, dtype)
 
 
+@pytest.mark.parametrize("n,k,c,dtype", [(3000, 12, 64, torch.float32), (9000, 16, 40, torch.bfloat16), (2000, 9, 260, torch.float32), (9000, 5, 3, torch.float16),
+                                         (20000, 3, 1024, torch.bfloat16), (700, 6, 64, torch.float32)])
+def test_walk_changes_no_bit(n, k, c, dtype):
+    """The bins' order of the points, the order reversed, and any order give what no order gives"""
+    rng = np.random.default_rng(n + k)
+    x, rs = W.uniform(n, 3, seed=k, sizes=[n - 11, 11])
+    binning = B.fg_bin_points(dev(x), dev(rs), k)
+    idx, d2 = B.fg_query_binned(binning, dev(rs), k)
+    rows, grad, w = values(rng, n, c, dtype), values(rng, n, c, dtype), torch.exp(-d2)
+    by = B.fg_index_sort(idx, n)
+    plain = (B.fg_combine(rows, idx, w), *B.fg_combine_backward(grad, rows, idx, w, sort=by))
+    for walk in (binning.perm, dev(np.arange(n, dtype=np.int32)[::-1]), dev(rng.permutation(n).astype(np.int32))):
+        got = (B.fg_combine(rows, idx, w, walk=walk), *B.fg_combine_backward(grad, rows, idx, w, sort=by, walk=walk))
+        assert all(torch.equal(a, b) for a, b in zip(got, plain))
+    # numbers outside are skipped, nothing is read or written there
+    out = torch.full((n, c), 7.0, dtype=dtype, device=DEV)
+    walk = binning.perm.clone()
+    left = walk[:4].long()
+    walk[:4] = dev(np.array([-1, n, 2 ** 31 - 1, -2 ** 31], dtype=np.int32))
+    B.fg_combine(rows, idx, w, out=out, walk=walk)
+    assert bool((out[left] == 7.0).all())
+    out[left] = plain[0][left]
+    assert torch.equal(out, plain[0])
+
+
 def test_gradients_against_differences():
     """Outputs are linear in rows and in weights: a step of 1 in one of them changes the loss by its gradient, but for rounding"""
     rng = np.random.default_rng(12)
@@ -519,7 +544,8 @@ def test_the_binding_checks_its_tensors():
            lambda: B.fg_lookup_backward(f, by), lambda: B.fg_lookup_backward(torch.zeros((12, 8), device=DEV), by, accumulate=True),
            lambda: B.fg_lookup_backward(torch.zeros((12, 8), device=DEV), by, grad_table=torch.zeros((5, 8), device=DEV)),
            lambda: B.fg_dispatch(f, i[:5]), lambda: B.fg_dispatch(f, i.reshape(-1)), lambda: B.fg_dispatch(f, i, torch.zeros((12, 7), device=DEV)),
-           lambda: B.fg_combine(f, i, w[:, :1]), lambda: B.fg_combine(f, i, w.half()), lambda: B.fg_combine(f, i, out=f[:5]),
+           lambda: B.fg_combine(f, i, walk=torch.zeros(5, dtype=torch.int32, device=DEV)), lambda: B.fg_combine(f, i, walk=torch.zeros(6, device=DEV)),
+           lambda: B.fg_combine_backward(f, f, i, w, sort=by, walk=i), lambda: B.fg_combine(f, i, w[:, :1]), lambda: B.fg_combine(f, i, w.half()), lambda: B.fg_combine(f, i, out=f[:5]),
            lambda: B.fg_combine_backward(f[:5], f, i, w), lambda: B.fg_combine_backward(f.half(), f, i, w),
            lambda: B.fg_combine_backward(f, f, i, w, sort=B.fg_index_sort(i, 7)), lambda: B.fg_combine_backward(f, f, i, w, grad_weights=w.half()),
            lambda: B.fg_combine_backward(f, f, i, w, grad_rows=f[:, :4])]

@@ -31,10 +31,10 @@ def call(kind, a):
     if kind == "dispatch":
         return lib.fg_dispatch(P(), i32(a["type"]), i64(a["t"]), i64(a["c"]), i64(a["c"]), P(), i32(a["k"]), i64(a["n"]), P(), i64(a["c"]), None)
     if kind == "combine":
-        return lib.fg_combine(P(), i32(a["type"]), i64(a["n"]), i64(a["c"]), i64(a["c"]), P(), P(), i64(a["t"]), i32(a["k"]), P(), i64(a["c"]), None)
+        return lib.fg_combine(P(), i32(a["type"]), i64(a["n"]), i64(a["c"]), i64(a["c"]), P(), P(), i64(a["t"]), i32(a["k"]), None, P(), i64(a["c"]), None)
     sort = P() if a["sorted"] else None
     return lib.fg_combine_backward(P(), i32(a["type"]), i64(a["t"]), i64(a["c"]), i64(a["c"]), P(), i64(a["n"]), i64(a["c"]), P(), P(), i32(a["k"]), sort, sort,
-                                   P(), i64(a["c"]), P(), P(), big, None)
+                                   sort, P(), i64(a["c"]), P(), P(), big, None)
 out = []
 for kind, a in json.loads(sys.stdin.read()):
     shim.shim_reset(0)

@@ -78,7 +78,7 @@ def test_dispatch(lib):
 
 def test_combine(lib):
     f = lib.fg_combine
-    ok = dict(rows=256, type=BF16, n=10, c=8, rs=8, index=8, w=8, t=5, k=2, out=256, os=8)
+    ok = dict(rows=256, type=BF16, n=10, c=8, rs=8, index=8, w=8, t=5, k=2, walk=None, out=256, os=8)
     call = lambda **k: f(*dict(ok, **k).values(), None)      # noqa: E731
     assert call(type=9) == call(rows=257) == call(out=257) == B.FG_ERR_UNSUPPORTED
     assert call(c=0) == call(rs=-1) == call(os=7) == call(t=-1) == call(k=0) == call(k=129) == call(n=-1) == call(t=N, k=2) == B.FG_ERR_BAD_SHAPE
@@ -91,7 +91,7 @@ def test_combine_backward(lib):
     assert need(10, 2, 8, BF16, None) == B.FG_ERR_NULL
     assert sizes(need, 10, 2, 8, 5)[0] == B.FG_ERR_UNSUPPORTED
     assert sizes(need, 10, 0, 8, BF16)[0] == sizes(need, N, 2, 8, BF16)[0] == sizes(need, 10, 2, 0, BF16)[0] == B.FG_ERR_BAD_SHAPE
-    ok = dict(grad=256, type=BF16, t=500, c=8, gs=8, rows=256, n=10, rs=8, index=8, w=8, k=2, order=8, bounds=8, gr=256, grs=8, gw=8, ws=256, bytes=1 << 30)
+    ok = dict(grad=256, type=BF16, t=500, c=8, gs=8, rows=256, n=10, rs=8, index=8, w=8, k=2, order=8, bounds=8, walk=None, gr=256, grs=8, gw=8, ws=256, bytes=1 << 30)
     call = lambda **k: f(*dict(ok, **k).values(), None)      # noqa: E731
     assert call(type=9) == call(grad=257) == call(rows=257) == call(gr=257) == B.FG_ERR_UNSUPPORTED
     assert call(c=0) == call(gs=-1) == call(rs=-1) == call(grs=7) == call(t=-1) == call(k=0) == call(k=129) == call(n=-1) == B.FG_ERR_BAD_SHAPE
