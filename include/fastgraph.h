@@ -294,7 +294,7 @@ fg_status fg_lookup(const void* table, int32_t type, int64_t n_rows, int64_t c, 
  *              accumulate != 0, the sums are added to what is there (float32, rounded once) and rows that no entry names are
  *              not touched
  * workspace: fg_lookup_backward_workspace_size() bytes, 256-byte aligned; may be NULL where that is 0. */
-fg_status fg_lookup_backward_workspace_size(int64_t m, int64_t c, int32_t type, size_t* bytes /* host out */);
+fg_status fg_lookup_backward_workspace_size(int64_t m, int64_t n_rows, int64_t c, int32_t type, size_t* bytes /* host out */);
 fg_status fg_lookup_backward(const void* grad_out, int32_t type, int64_t m, int64_t c, int64_t grad_stride, const int32_t* index,
                              const int32_t* order, const int32_t* bounds, int64_t n_rows, float scale, int32_t accumulate,
                              void* grad_table, int32_t grad_type, int64_t table_stride, void* workspace, size_t workspace_bytes,
@@ -328,7 +328,7 @@ fg_status fg_combine(const void* rows, int32_t type, int64_t n_rows, int64_t c, 
  * all of grad_rows is written.
  *   walk [n_rows] or NULL: with them, the order in which the rows of grad_rows are made, as for fg_combine; else without effect.
  * workspace (with order and grad_rows only): fg_combine_backward_workspace_size() bytes, 256-byte aligned; NULL where that is 0. */
-fg_status fg_combine_backward_workspace_size(int64_t t, int32_t k, int64_t c, int32_t type, size_t* bytes /* host out */);
+fg_status fg_combine_backward_workspace_size(int64_t t, int32_t k, int64_t n_rows, int64_t c, int32_t type, size_t* bytes /* host out */);
 fg_status fg_combine_backward(const void* grad_out, int32_t type, int64_t t, int64_t c, int64_t grad_stride, const void* rows,
                               int64_t n_rows, int64_t rows_stride, const int32_t* index, const float* weights, int32_t k,
                               const int32_t* order, const int32_t* bounds, const int32_t* walk, void* grad_rows,

@@ -94,11 +94,11 @@ def lib() -> ctypes.CDLL:
                 "fg_index_sort_workspace_size": [i64, i64, psz],
                 "fg_index_sort": [vp, i64, i64, vp, vp, vp, vp, sz, vp],
                 "fg_lookup": [vp, i32, i64, i64, i64, vp, i64, f32, vp, i64, vp],
-                "fg_lookup_backward_workspace_size": [i64, i64, i32, psz],
+                "fg_lookup_backward_workspace_size": [i64, i64, i64, i32, psz],
                 "fg_lookup_backward": [vp, i32, i64, i64, i64, vp, vp, vp, i64, f32, i32, vp, i32, i64, vp, sz, vp],
                 "fg_dispatch": [vp, i32, i64, i64, i64, vp, i32, i64, vp, i64, vp],
                 "fg_combine": [vp, i32, i64, i64, i64, vp, vp, i64, i32, vp, vp, i64, vp],
-                "fg_combine_backward_workspace_size": [i64, i32, i64, i32, psz],
+                "fg_combine_backward_workspace_size": [i64, i32, i64, i64, i32, psz],
                 "fg_combine_backward": [vp, i32, i64, i64, i64, vp, i64, i64, vp, vp, i32, vp, vp, vp, vp, i64, vp, vp, sz, vp]}.items():
             fn = getattr(L, name)
             fn.restype, fn.argtypes = ctypes.c_int, args
@@ -487,12 +487,12 @@ def fg_index_sort_workspace_size(m: int, n_rows: int) -> int:
     return _sizes("fg_index_sort_workspace_size", m, n_rows)
 
 
-def fg_lookup_backward_workspace_size(m: int, c: int, dtype: torch.dtype) -> int:
-    return _sizes("fg_lookup_backward_workspace_size", m, c, _TYPES[dtype])
+def fg_lookup_backward_workspace_size(m: int, n_rows: int, c: int, dtype: torch.dtype) -> int:
+    return _sizes("fg_lookup_backward_workspace_size", m, n_rows, c, _TYPES[dtype])
 
 
-def fg_combine_backward_workspace_size(t: int, k: int, c: int, dtype: torch.dtype) -> int:
-    return _sizes("fg_combine_backward_workspace_size", t, k, c, _TYPES[dtype])
+def fg_combine_backward_workspace_size(t: int, k: int, n_rows: int, c: int, dtype: torch.dtype) -> int:
+    return _sizes("fg_combine_backward_workspace_size", t, k, n_rows, c, _TYPES[dtype])
 
 
 class IndexSort:
@@ -571,9 +571,9 @@ def fg_lookup_backward(grad_out: torch.Tensor, sort: IndexSort, scale: float = 1
     if grad_table is None:
         if accumulate:
             raise ValueError("accumulate needs grad_table")
-        grad_table = torch.empty((sort.n_rows, c), dtype=dtype or grad_out.dtype, device=dev)
+        grad_table = grad_out.new_empty((sort.n_rows, c), dtype=dtype)
     to, to_stride = _row_view(grad_table, "grad_table", dtype, dev, (sort.n_rows, c))
-    ws = _scratch(workspace, fg_lookup_backward_workspace_size(m, c, grad_out.dtype), dev)
+    ws = _scratch(workspace, fg_lookup_backward_workspace_size(m, sort.n_rows, c, grad_out.dtype), dev)
     _call("fg_lookup_backward", dev, grad, _TYPES[grad_out.dtype], m, c, stride, index, sort._words.data_ptr(), sort._words.data_ptr() + 4 * m, sort.n_rows, scale,
           1 if accumulate else 0, to, _TYPES[grad_table.dtype], to_stride, _ptr(ws), _bytes(ws))
     return grad_table
@@ -641,7 +641,7 @@ def fg_combine_backward(grad_out: torch.Tensor, rows: torch.Tensor, index: torch
             raise ValueError("sort must be fg_index_sort's of index for %d rows" % n)
         order = sort._words.data_ptr()
         bounds = order + 4 * t * k
-        size = fg_combine_backward_workspace_size(t, k, c, rows.dtype)
+        size = fg_combine_backward_workspace_size(t, k, n, c, rows.dtype)
     if grad_rows is None:
         grad_rows = (torch.zeros if sort is None else torch.empty)((n, c), dtype=rows.dtype, device=dev)
     to, to_stride = _row_view(grad_rows, "grad_rows", rows.dtype, dev, (n, c))

@@ -572,13 +572,13 @@ fg_status fg_lookup(const void* table, int32_t type, int64_t n_rows, int64_t c, 
     return told(launch_lookup(type, {table, table_stride}, n_rows, c, index, m, scale, {out, out_stride}, (hipStream_t)stream));
 }
 
-fg_status fg_lookup_backward_workspace_size(int64_t m, int64_t c, int32_t type, size_t* bytes)
+fg_status fg_lookup_backward_workspace_size(int64_t m, int64_t n_rows, int64_t c, int32_t type, size_t* bytes)
 {
     if (!bytes) return FG_ERR_NULL;
     const fg_status st = check_rows(type, c);
     if (st != FG_OK) return st;
-    if (bad_count(m)) return FG_ERR_BAD_SHAPE;
-    *bytes = align_up(row_sums_workspace_bytes(type, m, c));
+    if (bad_count(m) || bad_count(n_rows)) return FG_ERR_BAD_SHAPE;
+    *bytes = align_up(row_sums_workspace_bytes(type, m, n_rows, c, false));
     return FG_OK;
 }
 
@@ -594,7 +594,7 @@ fg_status fg_lookup_backward(const void* grad_out, int32_t type, int64_t m, int6
     if (n_rows == 0) return FG_OK;
     if (!bounds || !grad_table || (m > 0 && (!grad_out || !index || !order))) return FG_ERR_NULL;
     if (misaligned(type, {grad_out}) || misaligned(grad_type, {grad_table})) return FG_ERR_UNSUPPORTED;
-    if (bad_workspace(workspace, workspace_bytes, row_sums_workspace_bytes(type, m, c))) return FG_ERR_WORKSPACE;
+    if (bad_workspace(workspace, workspace_bytes, row_sums_workspace_bytes(type, m, n_rows, c, false))) return FG_ERR_WORKSPACE;
     RowSums a = {};
     a.type = type; a.out_type = grad_type;
     a.grad = {grad_out, grad_stride}; a.out = {grad_table, table_stride};
@@ -628,13 +628,13 @@ fg_status fg_combine(const void* rows, int32_t type, int64_t n_rows, int64_t c, 
     return told(launch_combine(type, {rows, rows_stride}, n_rows, c, index, weights, t, k, walk, {out, out_stride}, (hipStream_t)stream));
 }
 
-fg_status fg_combine_backward_workspace_size(int64_t t, int32_t k, int64_t c, int32_t type, size_t* bytes)
+fg_status fg_combine_backward_workspace_size(int64_t t, int32_t k, int64_t n_rows, int64_t c, int32_t type, size_t* bytes)
 {
     if (!bytes) return FG_ERR_NULL;
     const fg_status st = check_rows(type, c);
     if (st != FG_OK) return st;
-    if (bad_fan(t, k)) return FG_ERR_BAD_SHAPE;
-    *bytes = align_up(row_sums_workspace_bytes(type, t * k, c));
+    if (bad_fan(t, k) || bad_count(n_rows)) return FG_ERR_BAD_SHAPE;
+    *bytes = align_up(row_sums_workspace_bytes(type, t * k, n_rows, c, sums_with_products(type, c)));
     return FG_OK;
 }
 
@@ -654,7 +654,7 @@ fg_status fg_combine_backward(const void* grad_out, int32_t type, int64_t t, int
     if (shared && (!bounds || (t > 0 && !order))) return FG_ERR_NULL;
     if (misaligned(type, {grad_out, rows, grad_rows})) return FG_ERR_UNSUPPORTED;
     const bool sums = shared && grad_rows && n_rows > 0, products = sums && t > 0 && grad_weights && sums_with_products(type, c);
-    if (sums && bad_workspace(workspace, workspace_bytes, row_sums_workspace_bytes(type, t * k, c))) return FG_ERR_WORKSPACE;
+    if (sums && bad_workspace(workspace, workspace_bytes, row_sums_workspace_bytes(type, t * k, n_rows, c, products))) return FG_ERR_WORKSPACE;
     if (sums) {
         RowSums a = {};
         a.type = type; a.out_type = type;

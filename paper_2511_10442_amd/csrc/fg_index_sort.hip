@@ -5,7 +5,7 @@
 // 64 entries at a time a wavefront finds, with one ballot for every bit of the digit, which lanes have the same digit; the number of
 // those before a lane is its rank, their count moves the wavefront's counter of that digit.
 //
-// Up to 8192 entries one workgroup sorts in LDS, all digits in one launch: 256 entries of 128 rows 4.1 us, 1000 of 5003 6.6.  Beyond, three launches a
+// Up to 8192 entries one workgroup sorts in LDS, all digits in one launch: 256 entries of 128 rows 3.2 us, 1000 of 5003 6.6.  Beyond, three launches a
 // digit (counts of the tiles, their prefix, the entries to their places) and one for the bounds: 262144 entries of 64 rows 15 us, 65536 of 131072 30
 // (latency: a tile's chain of loads, ranks and stores is 5 to 7 us, however few there are), 4M of 100k 82, 32M of 1M 720.  A pass over 4M moves 48 to 64 MB
 // in 23 to 26 us: stores of runs of 8 entries.
@@ -17,7 +17,9 @@ namespace {
 
 constexpr int kMaxBits = 10;                 // of a digit: a million rows in two passes
 constexpr int kSmallBlock = 1024;
-constexpr int64_t kSmallM = 8192;            // entries that one workgroup sorts in LDS (8192 of 50000 rows 18 us, with the launches for more 27)
+// Entries that one workgroup sorts in LDS (8192 of 50000 rows 18 us, with the launches for more 27): up to 256 a workgroup of 256 lanes (256 entries of
+// 128 rows 3.2 us, by 1024 lanes 4.1), beyond of 1024 (1000 of 5003 rows 6.6, by 256 lanes 10).
+constexpr int64_t kSmallM = 8192;
 // Rows whose bounds a workgroup writes; for more, more workgroups sort the same entries (1000 entries of 5003 rows: one workgroup and a search of the
 // bounds in a launch of its own 8.8 us, five 6.6).
 constexpr int64_t kSmallRows = 1024, kSmallBlocks = 256;
@@ -118,12 +120,12 @@ __device__ __forceinline__ W block_prefix(W x, W* sums)
 // ---- one workgroup -----------------------------------------------------------------------------------------------------
 
 // (of a large table every workgroup sorts all entries: the search of its share of the bounds finds them in LDS, and nothing is launched after it)
-template <int ITEMS>
-__global__ __launch_bounds__(kSmallBlock) void k_sort_small(const int32_t* __restrict__ index, int32_t m, uint32_t n_rows, int bits, int passes,
+template <int BLOCK, int ITEMS>
+__global__ __launch_bounds__(BLOCK) void k_sort_small(const int32_t* __restrict__ index, int32_t m, uint32_t n_rows, int bits, int passes,
                                                             int32_t* __restrict__ order, int32_t* __restrict__ place, int32_t* __restrict__ bounds)
 {
-    constexpr int kW = kSmallBlock / 64;
-    __shared__ uint32_t keys[ITEMS * kSmallBlock], from[ITEMS * kSmallBlock];
+    constexpr int kW = BLOCK / 64, kOwn = (1 << kMaxBits) / BLOCK;
+    __shared__ uint32_t keys[ITEMS * BLOCK], from[ITEMS * BLOCK];
     __shared__ uint32_t counter[kW][1 << kMaxBits];
     __shared__ uint32_t sums[kW];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -146,16 +148,31 @@ __global__ __launch_bounds__(kSmallBlock) void k_sort_small(const int32_t* __res
             rank[i] = rank_in_wave(counter[wave], (key[i] >> (pass * bits)) & (digits - 1), bits, e < m);
         }
         __syncthreads();
-        uint32_t count = 0;                                  // digits <= block
-        if (tid < digits)
-            for (int w = 0; w < kW; ++w) count += counter[w][tid];
-        uint32_t start = block_prefix<kW>(count, sums);
-        if (tid < digits)
-            for (int w = 0; w < kW; ++w) {
-                const uint32_t n = counter[w][tid];
-                counter[w][tid] = start;
-                start += n;
+        // (a wavefront's counters of one digit are read at once and written at once)
+        uint32_t before = 0;
+#pragma unroll
+        for (int o = 0; o < kOwn; ++o) {
+            if (o * BLOCK >= digits) break;
+            const int d = o * BLOCK + tid;
+            uint32_t n[kW], count = 0;
+#pragma unroll
+            for (int w = 0; w < kW; ++w) n[w] = d < digits ? counter[w][d] : 0;
+#pragma unroll
+            for (int w = 0; w < kW; ++w) count += n[w];
+            uint32_t start = before + block_prefix<kW>(count, sums);
+            if (d < digits)
+#pragma unroll
+                for (int w = 0; w < kW; ++w) {
+                    counter[w][d] = start;
+                    start += n[w];
+                }
+            if (kOwn > 1) {
+                if (tid == BLOCK - 1) sums[0] = start;
+                __syncthreads();
+                before = sums[0];
+                __syncthreads();
             }
+        }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
@@ -185,7 +202,7 @@ __global__ __launch_bounds__(kSmallBlock) void k_sort_small(const int32_t* __res
                 if (place) place[at[i]] = key[i] < n_rows ? e : -1;
             }
         }
-    for (int64_t v = (int64_t)blockIdx.x * kSmallBlock + tid; v <= n_rows; v += (int64_t)gridDim.x * kSmallBlock) {
+    for (int64_t v = (int64_t)blockIdx.x * BLOCK + tid; v <= n_rows; v += (int64_t)gridDim.x * BLOCK) {
         int lo = 0, hi = m;
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;
@@ -409,11 +426,11 @@ hipError_t many(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, 
     return hipSuccess;
 }
 
-template <int ITEMS>
+template <int BLOCK, int ITEMS>
 hipError_t small(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, int32_t* order, int32_t* place, int32_t* bounds, hipStream_t stream)
 {
     const int64_t blocks = (n_rows + kSmallRows) / kSmallRows;
-    FG_LAUNCH(k_sort_small<ITEMS>, dim3((unsigned)(blocks < kSmallBlocks ? blocks : kSmallBlocks)), dim3(kSmallBlock), 0, stream, index, (int32_t)m,
+    FG_LAUNCH((k_sort_small<BLOCK, ITEMS>), dim3((unsigned)(blocks < kSmallBlocks ? blocks : kSmallBlocks)), dim3(BLOCK), 0, stream, index, (int32_t)m,
               (uint32_t)n_rows, p.bits, p.passes, order, place, bounds);
     return hipSuccess;
 }
@@ -431,10 +448,10 @@ hipError_t launch_index_sort(const int32_t* index, int64_t m, int64_t n_rows, in
 {
     const Plan p = plan_for(m, n_rows);
     if (takes_small_sort(m)) {
-        if (m <= kSmallBlock) return small<1>(index, m, n_rows, p, order, place, bounds, stream);
-        if (m <= 2 * kSmallBlock) return small<2>(index, m, n_rows, p, order, place, bounds, stream);
-        if (m <= 4 * kSmallBlock) return small<4>(index, m, n_rows, p, order, place, bounds, stream);
-        return small<8>(index, m, n_rows, p, order, place, bounds, stream);
+        if (m <= kBlock) return small<kBlock, 1>(index, m, n_rows, p, order, place, bounds, stream);
+        if (m <= kSmallBlock) return small<kSmallBlock, 1>(index, m, n_rows, p, order, place, bounds, stream);
+        if (m <= 4 * kSmallBlock) return small<kSmallBlock, 4>(index, m, n_rows, p, order, place, bounds, stream);
+        return small<kSmallBlock, 8>(index, m, n_rows, p, order, place, bounds, stream);
     }
     if (!p.large) return many<kBlock, kItems>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);
     return many<kLargeBlock, kLargeItems>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);

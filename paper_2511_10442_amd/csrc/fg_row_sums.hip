@@ -203,10 +203,13 @@ __global__ __launch_bounds__(kBlock, DOTS && sizeof(T) == 2 ? 3 : 4) void k_row_
     });
 }
 
-// Few entries and rows: a wavefront for 64 pieces of a row; where a row has more than kAlone entries, the workgroup's wavefronts take a share of them
-// each and meet in LDS.  1000 tokens of 5003 x 257 float32, the commonest 80 times: 8 us (chunks and their join 5.8 + 6.0, and a launch).
-constexpr int kFewBlock = 1024, kAlone = 32;
-constexpr int64_t kFewEntries = 8192, kFewUnits = 32768;
+// Few entries, spread over many rows: a wavefront for 64 pieces of a row; where a row has more than kAlone entries after all, the workgroup's wavefronts
+// take a share of them each and meet in LDS.  Against chunks and their join, us (entries, rows x width): 1000 of 5003 x 257 float32 5.5 / 10.3, 500 of
+// 100 x 64 4.3 / 7.5, 100 of 30 x 512 3.3 / 4.6, 64 of 30000 x 256 10.5 / 11.3; but 1000 of 100 x 2048 17.9 / 15.3, 1000 of 3 x 300 21 / 10, 2000 of 2000 x
+// 4096 32 / 16.  (All 1000 of one row of many: 21 / 10.)
+constexpr int kFewBlock = 512, kAlone = 32;
+constexpr int64_t kFewEntries = 1024, kFewUnits = 32768;
+inline bool takes_few(int64_t m, int64_t n_rows, int64_t units) { return m <= kFewEntries && m <= 8 * n_rows && units <= kFewUnits; }
 template <typename T, int N, typename TO, bool WEIGHTED, bool ACCUMULATE>
 __global__ __launch_bounds__(kFewBlock) void k_row_sums_few(SumArgs a, const int32_t* __restrict__ order, const int32_t* __restrict__ bounds,
                                                             const float* __restrict__ weights, const T* __restrict__ grad, int64_t grad_stride,
@@ -319,7 +322,7 @@ hipError_t row_sums(const RowSums& r, const SumArgs& a, hipStream_t stream)
         d.waves = (pieces + 63) / 64;                        // a wavefront for 64 pieces whatever the width
         d.by_waves_far = DivideFar(d.waves);
         d.units = r.n_rows * d.waves;
-        if (r.m <= kFewEntries && d.units <= kFewUnits) {
+        if (takes_few(r.m, r.n_rows, d.units)) {
             FG_LAUNCH((k_row_sums_few<T, N, TO, WEIGHTED, ACCUMULATE>), blocks_for(d.units, kFewBlock / 64), dim3(kFewBlock), 0, stream, b, b.order, b.bounds,
                       b.weights, grad, r.grad.stride, (TO*)r.out.at, r.out.stride, d);
             return hipSuccess;
@@ -382,9 +385,11 @@ static int64_t elements_of_piece(int32_t type, int64_t c)
     return c >= n ? n : 1;
 }
 
-// (up to 64 pieces of a row are rounded up to a power of two: the lanes of a row with products)
-size_t row_sums_workspace_bytes(int32_t type, int64_t m, int64_t c)
+// (up to 64 pieces of a row are rounded up to a power of two: the lanes of a row with products; few entries and rows need none: k_row_sums_few, whose pieces
+// have four elements at least, or are one)
+size_t row_sums_workspace_bytes(int32_t type, int64_t m, int64_t n_rows, int64_t c, bool products)
 {
+    if (!products && takes_few(m, n_rows, n_rows * ((c + 255) / 256))) return 0;
     const int64_t n = elements_of_piece(type, c);
     int64_t pieces = (c + n - 1) / n;
     if (pieces <= 64) pieces = lanes_for(pieces);

@@ -56,7 +56,7 @@ struct RowSums {
 };
 // Widths of rows whose products with the summed rows, the weights' gradient, are made along with the sums.
 bool sums_with_products(int32_t type, int64_t c);
-size_t row_sums_workspace_bytes(int32_t type, int64_t m, int64_t c);
+size_t row_sums_workspace_bytes(int32_t type, int64_t m, int64_t n_rows, int64_t c, bool products);
 hipError_t launch_row_sums(const RowSums& a, hipStream_t stream);
 
 }  // namespace fg

@@ -47,8 +47,8 @@ def check_sort(index, n_rows, **kw):
         assert got.place is None
 
 
-# one workgroup with 1, 2, 4 and 8 entries a lane, many workgroups with 4 and 16; bounds from one workgroup, from the digits, by search
-@pytest.mark.parametrize("m", [0, 1, 63, 64, 65, 1024, 1025, 2048, 2049, 4096, 4097, 8192, 8193, 20011])
+# one workgroup of 256 lanes with 1 and 4 entries each, of 1024 with 4 and 8, many workgroups with 4 and 16; bounds from one workgroup, from the digits, by search
+@pytest.mark.parametrize("m", [0, 1, 63, 64, 65, 256, 257, 1024, 1025, 4096, 4097, 8192, 8193, 20011])
 @pytest.mark.parametrize("n_rows", [0, 1, 2, 7, 64, 1000, 1023, 1024, 4096, 4097, 70001])
 def test_sort(m, n_rows):
     rng = np.random.default_rng(m * 31 + n_rows)
@@ -170,7 +170,7 @@ def test_strided_rows_and_what_lies_between(dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("kind", ["uniform", "one", "frequent"])
-@pytest.mark.parametrize("m,n_rows,c", [(0, 5, 8), (1, 1, 1), (64, 3, 9), (127, 2, 40), (129, 1, 3), (1000, 700, 257), (9001, 40, 100), (5000, 9000, 36)])
+@pytest.mark.parametrize("m,n_rows,c", [(0, 5, 8), (1, 1, 1), (64, 3, 9), (127, 2, 40), (129, 1, 3), (1000, 700, 257), (1024, 128, 70), (1025, 4000, 24), (900, 300, 5), (9001, 40, 100), (5000, 9000, 36)])
 def test_lookup_backward(m, n_rows, c, kind, dtype):
     rng = np.random.default_rng(m + n_rows + c)
     index, grad = some_index(rng, (m,), n_rows, kind), values(rng, m, c, dtype)
@@ -554,7 +554,7 @@ def test_the_binding_checks_its_tensors():
             call()
     for call in [lambda: B.fg_index_sort(i, -1), lambda: B.fg_combine(f, torch.zeros((6, 129), dtype=torch.int32, device=DEV)),
                  lambda: B.fg_lookup_backward(torch.zeros((12, 8), device=DEV).half(), by, dtype=torch.bfloat16),
-                 lambda: B.fg_lookup_backward(torch.zeros((6400, 8), device=DEV), B.fg_index_sort(torch.zeros(6400, dtype=torch.int32, device=DEV), 6),
+                 lambda: B.fg_lookup_backward(torch.zeros((9000, 8), device=DEV), B.fg_index_sort(torch.zeros(9000, dtype=torch.int32, device=DEV), 6),
                                               workspace=torch.zeros(16, dtype=torch.uint8, device=DEV))]:
         with pytest.raises(B.FgError):
             call()

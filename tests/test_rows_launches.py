@@ -62,7 +62,8 @@ CHAINS = {
     "lookup": (("lookup", dict(type=BF16, n=1000, c=1024, m=500)), ["k_lookup"]),
     "lookup, narrow rows": (("lookup", dict(type=BF16, n=1000, c=7, m=500)), ["k_lookup"]),
     "lookup, past the caches": (("lookup", dict(type=BF16, n=1000, c=2048, m=1 << 17)), ["k_lookup"]),
-    "gradient, few entries": (("lookup_backward", dict(type=BF16, m=8192, c=512, n=5000)), ["k_row_sums_few"]),
+    "gradient, few entries": (("lookup_backward", dict(type=BF16, m=1024, c=512, n=5000)), ["k_row_sums_few"]),
+    "gradient, few entries of few rows": (("lookup_backward", dict(type=BF16, m=1024, c=512, n=100)), ROWS_OF_SUMS),
     "gradient, few entries of many rows": (("lookup_backward", dict(type=BF16, m=31, c=512, n=500000)), ["k_row_sums"]),
     "gradient, some": (("lookup_backward", dict(type=BF16, m=10000, c=512, n=5000)), ROWS_OF_SUMS),
     "gradient, many": (("lookup_backward", dict(type=F32, m=1 << 20, c=20, n=5000, acc=1)), ["k_row_sums", "k_row_parts", "k_row_join"]),
@@ -75,7 +76,7 @@ CHAINS = {
                                                          ["k_row_sums", "k_row_parts", "k_row_join"]),
     "combine's gradients, wide shared rows": (("combine_backward", dict(type=F32, t=9000, c=260, k=40, n=9000, sorted=1)),
                                               ["k_row_sums", "k_row_parts", "k_row_join", "k_combine_grad"]),
-    "combine's gradients, few wide shared rows": (("combine_backward", dict(type=F32, t=100, c=258, k=40, n=90, sorted=1)), ["k_row_sums_few", "k_combine_grad"]),
+    "combine's gradients, few wide shared rows": (("combine_backward", dict(type=F32, t=100, c=258, k=4, n=90, sorted=1)), ["k_row_sums_few", "k_combine_grad"]),
 }
 
 

@@ -52,10 +52,11 @@ def test_lookup(lib):
 
 def test_lookup_backward(lib):
     f, need = lib.fg_lookup_backward, lib.fg_lookup_backward_workspace_size
-    assert need(10, 8, BF16, None) == B.FG_ERR_NULL
-    assert sizes(need, 10, 8, 5)[0] == B.FG_ERR_UNSUPPORTED
-    assert sizes(need, 10, 0, BF16)[0] == sizes(need, -1, 8, BF16)[0] == sizes(need, N + 1, 8, BF16)[0] == B.FG_ERR_BAD_SHAPE
-    ok = dict(grad=256, type=BF16, m=1000, c=8, gs=8, index=8, order=8, bounds=8, n=5, scale=1.0, acc=0, to=256, gt=F32, ts=8, ws=256, bytes=1 << 30)
+    assert need(10, 5, 8, BF16, None) == B.FG_ERR_NULL
+    assert sizes(need, 10, 5, 8, 5)[0] == B.FG_ERR_UNSUPPORTED
+    assert sizes(need, 10, 5, 0, BF16)[0] == sizes(need, -1, 5, 8, BF16)[0] == sizes(need, N + 1, 5, 8, BF16)[0] == sizes(need, 10, -1, 8, BF16)[0] == B.FG_ERR_BAD_SHAPE
+    assert sizes(need, 1024, 5000, 512, BF16) == (B.FG_OK, 0) and sizes(need, 1025, 5000, 512, BF16)[1] >= 32 * 512 * 4
+    ok = dict(grad=256, type=BF16, m=10000, c=8, gs=8, index=8, order=8, bounds=8, n=5, scale=1.0, acc=0, to=256, gt=F32, ts=8, ws=256, bytes=1 << 30)
     call = lambda **k: f(*dict(ok, **k).values(), None)      # noqa: E731
     assert call(type=7) == call(gt=B.FG_F16) == call(type=F32, gt=BF16) == B.FG_ERR_UNSUPPORTED
     assert call(c=0) == call(gs=-1) == call(ts=7) == call(m=-1) == call(n=-1) == call(n=N + 1) == B.FG_ERR_BAD_SHAPE
@@ -88,9 +89,9 @@ def test_combine(lib):
 
 def test_combine_backward(lib):
     f, need = lib.fg_combine_backward, lib.fg_combine_backward_workspace_size
-    assert need(10, 2, 8, BF16, None) == B.FG_ERR_NULL
-    assert sizes(need, 10, 2, 8, 5)[0] == B.FG_ERR_UNSUPPORTED
-    assert sizes(need, 10, 0, 8, BF16)[0] == sizes(need, N, 2, 8, BF16)[0] == sizes(need, 10, 2, 0, BF16)[0] == B.FG_ERR_BAD_SHAPE
+    assert need(10, 2, 9, 8, BF16, None) == B.FG_ERR_NULL
+    assert sizes(need, 10, 2, 9, 8, 5)[0] == B.FG_ERR_UNSUPPORTED
+    assert sizes(need, 10, 0, 9, 8, BF16)[0] == sizes(need, N, 2, 9, 8, BF16)[0] == sizes(need, 10, 2, 9, 0, BF16)[0] == sizes(need, 10, 2, -1, 8, BF16)[0] == B.FG_ERR_BAD_SHAPE
     ok = dict(grad=256, type=BF16, t=500, c=8, gs=8, rows=256, n=10, rs=8, index=8, w=8, k=2, order=8, bounds=8, walk=None, gr=256, grs=8, gw=8, ws=256, bytes=1 << 30)
     call = lambda **k: f(*dict(ok, **k).values(), None)      # noqa: E731
     assert call(type=9) == call(grad=257) == call(rows=257) == call(gr=257) == B.FG_ERR_UNSUPPORTED
