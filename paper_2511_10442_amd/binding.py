@@ -496,7 +496,7 @@ def fg_combine_backward_workspace_size(t: int, k: int, n_rows: int, c: int, dtyp
 
 
 class IndexSort:
-    """An index in the order of the rows that it names (fg_index_sort)."""
+    """An index in the order of the rows that it names (fg_index_sort).  It goes with the index's values: sort again after changing them."""
     __slots__ = ("index", "n_rows", "_words", "_place", "_views")
 
     def __init__(self, index: torch.Tensor, n_rows: int, words: torch.Tensor, place: bool):

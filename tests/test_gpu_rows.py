@@ -366,6 +366,56 @@ def test_walk_changes_no_bit(n, k, c, dtype):
     assert torch.equal(out, plain[0])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("c", [70001, 262144])
+def test_wide_rows(c, dtype):
+    """Up to the largest width: many wavefronts a row"""
+    rng = np.random.default_rng(c)
+    n, t, k = 7, 5, 3
+    index, w = some_index(rng, (t, k), n), dev(rng.random((t, k)).astype(np.float32))
+    rows, grad = values(rng, n, c, dtype), values(rng, t, c, dtype)
+    got = B.fg_lookup(rows, dev(index.reshape(-1)), 0.5)
+    ref = R.lookup(R.wide(rows), index.reshape(-1), 0.5)
+    R.check(got, ref, abs(ref), 0, dtype)
+    ref, mass = R.combine(R.wide(rows), index, R.wide(w))
+    R.check(B.fg_combine(rows, dev(index), w), ref, mass, k, dtype)
+    by = B.fg_index_sort(dev(index), n)
+    sums, mass, count = R.row_sums(R.wide(grad), index, R.wide(w), n)
+    dots = R.dots(R.wide(grad), R.wide(rows), index)
+    got, gw = B.fg_combine_backward(grad, rows, dev(index), w, sort=by)
+    R.check(got, sums, mass, count[:, None], dtype)
+    R.check(gw, *dots, c, torch.float32)
+    sent = B.fg_dispatch(grad, by.place, torch.zeros((t * k, c), dtype=dtype, device=DEV))
+    place = by.place.cpu().numpy()
+    for (i, j), p in np.ndenumerate(place):
+        assert p < 0 or torch.equal(sent[p], grad[i])
+    with pytest.raises(B.FgError):
+        B.fg_lookup(torch.zeros((2, 262145), device=DEV), dev(index))
+
+
+def test_nothing_to_do():
+    """No tokens, no rows: outputs that are there are written all the same"""
+    none, rows = torch.zeros((0, 3), dtype=torch.int32, device=DEV), torch.ones((6, 8), device=DEV)
+    empty, w = torch.zeros((0, 8), device=DEV), torch.zeros((0, 3), device=DEV)
+    assert B.fg_combine(rows, none, w).shape == (0, 8) and B.fg_dispatch(empty, none).shape == (0, 8)
+    by = B.fg_index_sort(none, 6)
+    assert by.place.shape == (0, 3) and by.order.numel() == 0 and not bool(by.bounds.any())
+    for sort in (by, None):
+        got, gw = B.fg_combine_backward(empty, rows, none, w, sort=sort)
+        assert got.shape == (6, 8) and not bool(got.any()) and gw.shape == (0, 3)
+    assert not bool(B.fg_lookup_backward(empty, B.fg_index_sort(torch.zeros(0, dtype=torch.int32, device=DEV), 6)).any())
+    # no rows to name
+    index, grad, w = torch.zeros((4, 3), dtype=torch.int32, device=DEV), torch.ones((4, 8), device=DEV), torch.ones((4, 3), device=DEV)
+    by = B.fg_index_sort(index, 0)
+    assert bool((by.place == -1).all()) and by.bounds.tolist() == [0] and by.order.tolist() == list(range(12))
+    assert not bool(B.fg_combine(empty, index, w).any())
+    for sort in (by, None):
+        got, gw = B.fg_combine_backward(grad, empty, index, w, sort=sort)
+        assert got.shape == (0, 8) and not bool(gw.any())
+    assert B.fg_lookup_backward(grad.repeat(3, 1), by).shape == (0, 8)
+    torch.cuda.synchronize()
+
+
 def test_gradients_against_differences():
     """Outputs are linear in rows and in weights: a step of 1 in one of them changes the loss by its gradient, but for rounding"""
     rng = np.random.default_rng(12)
