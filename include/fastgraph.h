@@ -302,7 +302,7 @@ fg_status fg_lookup_backward(const void* grad_out, int32_t type, int64_t m, int6
 
 /* Rows into the order of an index with k entries a row: out[place[i][j]] = x[i], bit for bit.
  *   x [t][c], place [t][k] (fg_index_sort's of the choices [t][k]: expert e's rows are then out[bounds[e] .. bounds[e+1])),
- *   out [n_rows][c].  Rows of out that no entry names are left as they were; a row named twice gets one of the two.
+ *   out [n_rows][c].  Rows of out that no entry names are left as they were; of a row named twice every element is one of the two.
  * The gradient of x is fg_combine of the gradient of out by `place`, without weights. */
 fg_status fg_dispatch(const void* x, int32_t type, int64_t t, int64_t c, int64_t x_stride, const int32_t* place, int32_t k,
                       int64_t n_rows, void* out, int64_t out_stride, void* stream);
@@ -323,8 +323,8 @@ fg_status fg_combine(const void* rows, int32_t type, int64_t n_rows, int64_t c, 
  *   grad_weights[i][j] = <grad_out[i], rows[index[i][j]]>, 0 where the entry names no row
  *   grad_out [t][c], rows [n_rows][c] (read for grad_weights only), grad_rows [n_rows][c] or NULL, grad_weights [t][k] or NULL;
  *   rows of grad_out, rows and grad_rows are of `type`.
- * order, bounds: both NULL: no row is named twice (index = place); rows that no entry names are left as they were, and a row that
- * is named twice gets one of its terms.  Both given (fg_index_sort of index [t*k]): rows may be named any number of times, and
+ * order, bounds: both NULL: no row is named twice (index = place); rows that no entry names are left as they were, and of a row
+ * that is named twice every element is one of its terms.  Both given (fg_index_sort of index [t*k]): rows may be named any number of times, and
  * all of grad_rows is written.
  *   walk [n_rows] or NULL: with them, the order in which the rows of grad_rows are made, as for fg_combine; else without effect.
  * workspace (with order and grad_rows only): fg_combine_backward_workspace_size() bytes, 256-byte aligned; NULL where that is 0. */

@@ -19,7 +19,7 @@ constexpr int64_t kFill = 256 * 2048;        // lanes that the chip holds at a t
 // Eight workgroups for every place on the chip; more work than that: they take several turns.  Where pieces differ in what they take, a workgroup that is
 // done makes room for the next instead (64k tokens' gradient, the commonest 4000 times: 313 us in turns, 300 so).
 constexpr int64_t kMostBlocks = 1 << 14, kMostUneven = 1 << 20;
-// Times that a row is named, on average, from which on rows are expected to be found in an XCD's L2 by those that name them too (kShared: by_xcd)
+// Times that a row is named, on average, from which on rows are expected to be found in an XCD's L2 by those that name them too (by_xcd)
 constexpr int64_t kShared = 4;
 constexpr int64_t kFewWaves = 256 * 16;      // half of the wavefronts that the chip holds
 // Bytes that a call moves, twice the last-level cache, from which on most of its output has left that cache when the call ends: it is stored past the

@@ -9,8 +9,8 @@ namespace {
 // ---- sums over the entries of a row ------------------------------------------------------------------------------------
 
 // Rows that are named often are summed in parts: `chunk` entries of the sorted index that all name one row, and kChunks such chunks, are summed
-// by themselves and put together afterwards, so that what one lane does for a row hardly grows with the row's entries.  chunk is kChunk,
-// or, for rows of a graph are named often, but all of them, and as chunks they would be read by a few scattered lanes, four times the mean of a row's
+// by themselves and put together afterwards, so that what one lane does for a row hardly grows with the row's entries.  chunk is kChunk.  Rows of a
+// graph are all named often, and as chunks they would be read by a few scattered lanes: there it grows to four times the mean of a row's
 // entries, as far as the rows alone give 512 lanes for every entry of a chunk, so that one lane's share stays small beside the whole (a power of two;
 // 20k points, 40 neighbours of 64 float32: 57 us with chunks of 32, 42 with 256; 9k points, 100 neighbours of 128 78 and 50; but entries whose rows follow
 // Zipf's law, 1M of 5000 rows of 64 bf16, 308 us with 64 lanes, 90 with 256, 62 so; 66k of 105 rows of 2112 147, 90, 80).
@@ -120,8 +120,8 @@ __device__ __forceinline__ bool one_row(const SumArgs& a, int32_t p, int32_t n, 
 // (bounds that are no fg_index_sort's: nothing outside is read)
 __device__ __forceinline__ void within(const SumArgs& a, int32_t& from, int32_t& to)
 {
-    from = from < 0 ? 0 : from;
-    to = to > a.m ? a.m : to;
+    from = from < 0 ? 0 : (from > a.m ? a.m : from);
+    to = to < 0 ? 0 : (to > a.m ? a.m : to);
 }
 __device__ __forceinline__ int32_t first_chunk(const SumArgs& a, int32_t from) { return (int32_t)(((int64_t)from + (1 << a.shift) - 1) >> a.shift); }
 

@@ -477,6 +477,54 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(table[at.long()], grad[:, None, :].expand(t, k, c))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("c", [72, 1000, 2049, 4104])
+def test_more_than_the_caches_hold(c, dtype):
+    """Calls that move 512 MB and more against the same rows in calls of a seventh: where a sum does not go by the number of rows, to the bit"""
+    gen = torch.Generator(device=DEV).manual_seed(c)
+    size, k = torch.empty((), dtype=dtype).element_size(), 3
+    m = (512 << 20) // (c * size) + 77
+    t = m // k
+
+    def part(n, i):
+        return slice(n * i // 7, n * (i + 1) // 7)
+    table = torch.randn((5001, c), generator=gen, device=DEV).to(dtype)
+    index = torch.randint(-1, 5002, (m,), generator=gen, device=DEV, dtype=torch.int32)
+    got = B.fg_lookup(table, index, 0.7)
+    assert all(torch.equal(got[part(m, i)], B.fg_lookup(table, index[part(m, i)], 0.7)) for i in range(7))
+    # every row named once, a few by nobody
+    rows, grad = torch.randn((m, c), generator=gen, device=DEV).to(dtype), torch.randn((t, c), generator=gen, device=DEV).to(dtype)
+    at = torch.randperm(m, generator=gen, device=DEV)[:t * k].to(torch.int32).view(t, k)
+    at[::50] = -1
+    w = torch.rand((t, k), generator=gen, device=DEV)
+    for weights in (w, None):
+        got = B.fg_combine(rows, at, weights)
+        assert all(torch.equal(got[part(t, i)], B.fg_combine(rows, at[part(t, i)], None if weights is None else weights[part(t, i)])) for i in range(7))
+    got, gw = B.fg_combine_backward(grad, rows, at, w)
+    again, parts = torch.zeros_like(rows), []
+    for i in range(7):
+        parts.append(B.fg_combine_backward(grad[part(t, i)], rows, at[part(t, i)], w[part(t, i)], grad_rows=again)[1])
+    assert torch.equal(got, again)
+    # (products go by the lanes that a token gets, and these by the number of tokens)
+    terms = [torch.where(at[:, j:j + 1] >= 0, rows[at[:, j].clamp(0).long()].double() * grad.double(), 0.0) for j in range(k)]
+    ref, mass = R.wide(torch.stack([x.sum(1) for x in terms], 1)), R.wide(torch.stack([x.abs().sum(1) for x in terms], 1))
+    R.check(gw, ref, mass, c, torch.float32)
+    R.check(torch.cat(parts), ref, mass, c, torch.float32)
+    # a table of which most rows are named by nobody or a few, one by many
+    n, few = m, 3001
+    index = torch.randint(-1, n, (few,), generator=gen, device=DEV, dtype=torch.int32)
+    index[::9] = n // 2
+    grad = torch.randn((few, c), generator=gen, device=DEV).to(dtype)
+    named = index >= 0
+    count = torch.zeros(n, device=DEV, dtype=torch.float64).index_add_(0, index[named].long(), torch.ones(int(named.sum()), device=DEV, dtype=torch.float64))
+    some = torch.nonzero(count)[:, 0]
+    to = torch.cumsum(count > 0, 0) - 1
+    ref, mass = (torch.zeros((len(some), c), device=DEV, dtype=torch.float64).index_add_(0, to[index[named].long()], x) for x in (grad[named].double(), grad[named].double().abs()))
+    got = B.fg_lookup_backward(grad, B.fg_index_sort(index, n))
+    assert int(torch.count_nonzero(got.view(torch.int32 if dtype == torch.float32 else torch.int16).any(1))) <= len(some)
+    R.check(got[some], R.wide(ref), R.wide(mass), count[some, None].cpu().numpy(), dtype)
+
+
 def test_on_a_stream_of_its_own():
     rng = np.random.default_rng(1)
     index, x, w = dev(choices(rng, 500, 4, 16, 0.1)), values(rng, 500, 320, torch.bfloat16), dev(rng.random((500, 4)).astype(np.float32))
