@@ -5,7 +5,7 @@
 // 64 entries at a time a wavefront finds, with one ballot for every bit of the digit, which lanes have the same digit; the number of
 // those before a lane is its rank, their count moves the wavefront's counter of that digit.
 //
-// Up to 8192 entries one workgroup sorts in LDS, all digits in one launch: 256 entries of 128 rows 3.2 us, 1000 of 5003 6.6.  Beyond, three launches a
+// A few entries are not sorted but counted: k_sort_few.  Up to 8192 one workgroup sorts in LDS, all digits in one launch.  Beyond, three launches a
 // digit (counts of the tiles, their prefix, the entries to their places) and one for the bounds: 262144 entries of 64 rows 15 us, 65536 of 131072 30
 // (latency: a tile's chain of loads, ranks and stores is 5 to 7 us, however few there are), 4M of 100k 82, 32M of 1M 720.  A pass over 4M moves 48 to 64 MB
 // in 23 to 26 us: stores of runs of 8 entries.
@@ -17,11 +17,14 @@ namespace {
 
 constexpr int kMaxBits = 10;                 // of a digit: a million rows in two passes
 constexpr int kSmallBlock = 1024;
-// Entries that one workgroup sorts in LDS (8192 of 50000 rows 18 us, with the launches for more 27): up to 256 a workgroup of 256 lanes (256 entries of
-// 128 rows 3.2 us, by 1024 lanes 4.1), beyond of 1024 (1000 of 5003 rows 6.6, by 256 lanes 10).
+// Entries that one workgroup sorts in LDS (8192 of 50000 rows 18 us, with the launches for more 27)
 constexpr int64_t kSmallM = 8192;
-// Rows whose bounds a workgroup writes; for more, more workgroups sort the same entries (1000 entries of 5003 rows: one workgroup and a search of the
-// bounds in a launch of its own 8.8 us, five 6.6).
+// Entries that are counted, by 4 and by 16 lanes a question, and how many questions (entries and bounds) and looks at a key at most.  us counted by 4 / counted by 16 / sorted
+// in LDS: 64 entries of 8 rows 1.7 / 2.1 / 3.0, 300 of 50000 4.2 / 5.3 / 7.0, 100 of 200000 5.5 / 8.6 / 7.9, 1000 of 5003 7.2 / 4.0 / 7.2, 1024 of 20000
+// 7.2 / 5.5 / 7.5, 1000 of 60000 7.7 / 8.3 / 7.6, 4096 of 10000 21 / 8.4 / 12.4, of 16000 21 / 12.0 / 12.5.  (8192 of 256 by 16 13.1, in LDS 14.6.)
+constexpr int64_t kFewM = 512, kFewQuestions = 1 << 18, kSomeM = 4096, kSomeQuestions = 1 << 15, kSomeLooks = 1 << 26;
+// Rows whose bounds a workgroup writes; for more, more workgroups sort the same entries (1000 entries of 5003 rows, before they were
+// counted: one workgroup and a search of the bounds in a launch of its own 8.8 us, five 6.6).
 constexpr int64_t kSmallRows = 1024, kSmallBlocks = 256;
 constexpr int kBlock = 256;
 constexpr unsigned kXcds = 8;
@@ -64,6 +67,8 @@ inline Layout layout_for(int64_t m, const Plan& p)
     return l;
 }
 
+inline bool takes_few(int64_t m, int64_t n_rows) { return m <= kFewM && m + n_rows < kFewQuestions; }
+inline bool takes_some(int64_t m, int64_t n_rows) { return m <= kSomeM && m + n_rows < kSomeQuestions && m * (m + n_rows) < kSomeLooks; }
 inline bool takes_small_sort(int64_t m) { return m <= kSmallM; }
 
 __device__ __forceinline__ uint32_t key_of(int32_t name, uint32_t n_rows) { return (uint32_t)name < n_rows ? (uint32_t)name : n_rows; }
@@ -117,14 +122,61 @@ __device__ __forceinline__ W block_prefix(W x, W* sums)
     return before + run - x;
 }
 
+// ---- a few entries, counted ----------------------------------------------------------------------------------------------
+
+// An entry's place is the number of entries before it, a row's bound that of the entries of rows before it: LANES lanes a question look at every key, which has
+// the entry's number in its `low` lowest bits (up to 512 entries and 2^18 rows, 4096 and 2^15: 27 bits), in LDS.  No step waits for another but the first load.
+constexpr int kFewBlock = 1024;
+template <int LANES>
+__global__ __launch_bounds__(kFewBlock) void k_sort_few(const int32_t* __restrict__ index, int32_t m, uint32_t n_rows, int low, int32_t* __restrict__ order,
+                                                        int32_t* __restrict__ place, int32_t* __restrict__ bounds)
+{
+    typedef uint32_t Four __attribute__((ext_vector_type(4)));
+    extern __shared__ Four fours[];                      // as many as LANES divides
+    uint32_t* keys = (uint32_t*)fours;
+    const int tid = threadIdx.x, sub = tid % LANES, n = (m + 4 * LANES - 1) / (4 * LANES) * LANES;
+    for (int e = tid; e < 4 * n; e += kFewBlock) keys[e] = e < m ? key_of(index[e], n_rows) << low | e : ~0u;
+    __syncthreads();
+    const int64_t q = (int64_t)blockIdx.x * (kFewBlock / LANES) + tid / LANES;
+    if (q > m + (int64_t)n_rows) return;
+    const uint32_t what = q < m ? keys[q] : (uint32_t)(q - m) << low;
+    uint32_t before = 0;
+#pragma unroll 4
+    for (int i = sub; i < n; i += LANES) {
+        const Four k = fours[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) before += k[j] < what;
+    }
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) before += __shfl_xor(before, o);
+    if (sub != 0) return;
+    if (q >= m) bounds[q - m] = (int32_t)before;
+    else {
+        order[before] = (int32_t)q;
+        if (place) place[q] = what >> low < n_rows ? (int32_t)before : -1;
+    }
+}
+
+template <int LANES>
+hipError_t count_few(const int32_t* index, int64_t m, int64_t n_rows, int32_t* order, int32_t* place, int32_t* bounds, hipStream_t stream)
+{
+    int low = 0;
+    while (((int64_t)1 << low) < m) ++low;
+    const int64_t each = kFewBlock / LANES, blocks = (m + n_rows + each) / each;
+    const size_t lds = (size_t)(m + 4 * LANES - 1) / (4 * LANES) * (4 * LANES) * sizeof(uint32_t);
+    FG_LAUNCH((k_sort_few<LANES>), dim3((unsigned)blocks), dim3(kFewBlock), lds, stream, index, (int32_t)m, (uint32_t)n_rows, low, order, place, bounds);
+    return hipSuccess;
+}
+
 // ---- one workgroup -----------------------------------------------------------------------------------------------------
 
 // (of a large table every workgroup sorts all entries: the search of its share of the bounds finds them in LDS, and nothing is launched after it)
-template <int BLOCK, int ITEMS>
-__global__ __launch_bounds__(BLOCK) void k_sort_small(const int32_t* __restrict__ index, int32_t m, uint32_t n_rows, int bits, int passes,
+template <int ITEMS>
+__global__ __launch_bounds__(kSmallBlock) void k_sort_small(const int32_t* __restrict__ index, int32_t m, uint32_t n_rows, int bits, int passes,
                                                             int32_t* __restrict__ order, int32_t* __restrict__ place, int32_t* __restrict__ bounds)
 {
-    constexpr int kW = BLOCK / 64, kOwn = (1 << kMaxBits) / BLOCK;
+    constexpr int BLOCK = kSmallBlock, kW = BLOCK / 64;
+    static_assert(1 << kMaxBits <= BLOCK, "a lane has one digit at most");
     __shared__ uint32_t keys[ITEMS * BLOCK], from[ITEMS * BLOCK];
     __shared__ uint32_t counter[kW][1 << kMaxBits];
     __shared__ uint32_t sums[kW];
@@ -149,30 +201,18 @@ __global__ __launch_bounds__(BLOCK) void k_sort_small(const int32_t* __restrict_
         }
         __syncthreads();
         // (a wavefront's counters of one digit are read at once and written at once)
-        uint32_t before = 0;
+        uint32_t n[kW], count = 0;
 #pragma unroll
-        for (int o = 0; o < kOwn; ++o) {
-            if (o * BLOCK >= digits) break;
-            const int d = o * BLOCK + tid;
-            uint32_t n[kW], count = 0;
+        for (int w = 0; w < kW; ++w) n[w] = tid < digits ? counter[w][tid] : 0;
 #pragma unroll
-            for (int w = 0; w < kW; ++w) n[w] = d < digits ? counter[w][d] : 0;
+        for (int w = 0; w < kW; ++w) count += n[w];
+        uint32_t start = block_prefix<kW>(count, sums);
+        if (tid < digits)
 #pragma unroll
-            for (int w = 0; w < kW; ++w) count += n[w];
-            uint32_t start = before + block_prefix<kW>(count, sums);
-            if (d < digits)
-#pragma unroll
-                for (int w = 0; w < kW; ++w) {
-                    counter[w][d] = start;
-                    start += n[w];
-                }
-            if (kOwn > 1) {
-                if (tid == BLOCK - 1) sums[0] = start;
-                __syncthreads();
-                before = sums[0];
-                __syncthreads();
+            for (int w = 0; w < kW; ++w) {
+                counter[w][tid] = start;
+                start += n[w];
             }
-        }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
@@ -426,11 +466,11 @@ hipError_t many(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, 
     return hipSuccess;
 }
 
-template <int BLOCK, int ITEMS>
+template <int ITEMS>
 hipError_t small(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, int32_t* order, int32_t* place, int32_t* bounds, hipStream_t stream)
 {
     const int64_t blocks = (n_rows + kSmallRows) / kSmallRows;
-    FG_LAUNCH((k_sort_small<BLOCK, ITEMS>), dim3((unsigned)(blocks < kSmallBlocks ? blocks : kSmallBlocks)), dim3(BLOCK), 0, stream, index, (int32_t)m,
+    FG_LAUNCH((k_sort_small<ITEMS>), dim3((unsigned)(blocks < kSmallBlocks ? blocks : kSmallBlocks)), dim3(kSmallBlock), 0, stream, index, (int32_t)m,
               (uint32_t)n_rows, p.bits, p.passes, order, place, bounds);
     return hipSuccess;
 }
@@ -447,11 +487,12 @@ hipError_t launch_index_sort(const int32_t* index, int64_t m, int64_t n_rows, in
                              hipStream_t stream)
 {
     const Plan p = plan_for(m, n_rows);
+    if (takes_few(m, n_rows)) return count_few<4>(index, m, n_rows, order, place, bounds, stream);
+    if (takes_some(m, n_rows)) return count_few<16>(index, m, n_rows, order, place, bounds, stream);
     if (takes_small_sort(m)) {
-        if (m <= kBlock) return small<kBlock, 1>(index, m, n_rows, p, order, place, bounds, stream);
-        if (m <= kSmallBlock) return small<kSmallBlock, 1>(index, m, n_rows, p, order, place, bounds, stream);
-        if (m <= 4 * kSmallBlock) return small<kSmallBlock, 4>(index, m, n_rows, p, order, place, bounds, stream);
-        return small<kSmallBlock, 8>(index, m, n_rows, p, order, place, bounds, stream);
+        if (m <= kSmallBlock) return small<1>(index, m, n_rows, p, order, place, bounds, stream);
+        if (m <= 4 * kSmallBlock) return small<4>(index, m, n_rows, p, order, place, bounds, stream);
+        return small<8>(index, m, n_rows, p, order, place, bounds, stream);
     }
     if (!p.large) return many<kBlock, kItems>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);
     return many<kLargeBlock, kLargeItems>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);

@@ -47,9 +47,9 @@ def check_sort(index, n_rows, **kw):
         assert got.place is None
 
 
-# one workgroup of 256 lanes with 1 and 4 entries each, of 1024 with 4 and 8, many workgroups with 4 and 16; bounds from one workgroup, from the digits, by search
-@pytest.mark.parametrize("m", [0, 1, 63, 64, 65, 256, 257, 1024, 1025, 4096, 4097, 8192, 8193, 20011])
-@pytest.mark.parametrize("n_rows", [0, 1, 2, 7, 64, 1000, 1023, 1024, 4096, 4097, 70001])
+# counted by 4 lanes and by 16, one workgroup with 1, 4 and 8 entries a lane, many workgroups with 4; bounds from the keys, from the digits, by search
+@pytest.mark.parametrize("m", [0, 1, 63, 64, 65, 256, 257, 512, 513, 1024, 1025, 4096, 4097, 8192, 8193, 20011])
+@pytest.mark.parametrize("n_rows", [0, 1, 2, 7, 64, 1000, 1023, 1024, 4096, 4097, 12287, 12288, 31743, 31744, 70001, 261631, 261632])
 def test_sort(m, n_rows):
     rng = np.random.default_rng(m * 31 + n_rows)
     for kind in ("uniform", "one", "frequent"):

@@ -53,7 +53,13 @@ ROWS_OF_SUMS = ["k_row_sums", "k_row_join"]
 PASS = ["k_sort_count", "k_sort_scan", "k_sort_scatter"]
 # (the calls, and the kernels that serve them)
 CHAINS = {
-    "a few entries": (("sort", dict(m=8192, n=100000)), ["k_sort_small"]),
+    "a few entries": (("sort", dict(m=512, n=(1 << 18) - 513)), ["k_sort_few"]),
+    "a few entries of more rows": (("sort", dict(m=512, n=(1 << 18) - 512)), ["k_sort_small"]),
+    "some entries": (("sort", dict(m=4096, n=(1 << 14) - 4097)), ["k_sort_few"]),
+    "some entries, more rows": (("sort", dict(m=1024, n=(1 << 15) - 1025)), ["k_sort_few"]),
+    "some entries, still more rows": (("sort", dict(m=1024, n=(1 << 15) - 1024)), ["k_sort_small"]),
+    "some entries of more rows": (("sort", dict(m=4096, n=(1 << 14) - 4096)), ["k_sort_small"]),
+    "entries that one workgroup sorts": (("sort", dict(m=8192, n=100000)), ["k_sort_small"]),
     "one digit": (("sort", dict(m=8193, n=1023)), PASS),
     "two digits": (("sort", dict(m=100000, n=1024)), PASS * 2 + ["k_sort_bounds"]),
     "two digits, many entries": (("sort", dict(m=1 << 21, n=(1 << 20) - 1)), PASS * 2 + ["k_sort_bounds"]),
