@@ -488,11 +488,11 @@ def fg_index_sort_workspace_size(m: int, n_rows: int) -> int:
 
 
 def fg_lookup_backward_workspace_size(m: int, n_rows: int, c: int, dtype: torch.dtype) -> int:
-    return _sizes("fg_lookup_backward_workspace_size", m, n_rows, c, _TYPES[dtype])
+    return _sizes("fg_lookup_backward_workspace_size", m, n_rows, c, _TYPES.get(dtype, -1))
 
 
 def fg_combine_backward_workspace_size(t: int, k: int, n_rows: int, c: int, dtype: torch.dtype) -> int:
-    return _sizes("fg_combine_backward_workspace_size", t, k, n_rows, c, _TYPES[dtype])
+    return _sizes("fg_combine_backward_workspace_size", t, k, n_rows, c, _TYPES.get(dtype, -1))
 
 
 class IndexSort:
@@ -572,10 +572,13 @@ def fg_lookup_backward(grad_out: torch.Tensor, sort: IndexSort, scale: float = 1
         if accumulate:
             raise ValueError("accumulate needs grad_table")
         grad_table = grad_out.new_empty((sort.n_rows, c), dtype=dtype)
-    to, to_stride = _row_view(grad_table, "grad_table", dtype, dev, (sort.n_rows, c))
+        to, to_stride = grad_table.data_ptr() or None, c
+    else:
+        to, to_stride = _row_view(grad_table, "grad_table", dtype, dev, (sort.n_rows, c))
     ws = _scratch(workspace, fg_lookup_backward_workspace_size(m, sort.n_rows, c, grad_out.dtype), dev)
-    _call("fg_lookup_backward", dev, grad, _TYPES[grad_out.dtype], m, c, stride, index, sort._words.data_ptr(), sort._words.data_ptr() + 4 * m, sort.n_rows, scale,
-          1 if accumulate else 0, to, _TYPES[grad_table.dtype], to_stride, _ptr(ws), _bytes(ws))
+    order = sort._words.data_ptr()
+    _call("fg_lookup_backward", dev, grad, _TYPES[grad_out.dtype], m, c, stride, index, order, order + 4 * m, sort.n_rows, scale, 1 if accumulate else 0,
+          to, _TYPES.get(grad_table.dtype, -1), to_stride, _ptr(ws), _bytes(ws))
     return grad_table
 
 
@@ -590,7 +593,7 @@ def fg_dispatch(x: torch.Tensor, place: torch.Tensor, out: torch.Tensor | None =
         raise ValueError("place must be [%d, k]" % x.shape[0])
     c = x.shape[1]
     if out is None:
-        out = torch.empty((t * k, c), dtype=x.dtype, device=dev)
+        out = x.new_empty((t * k, c))
     to, to_stride = _row_view(out, "out", x.dtype, dev, (out.shape[0], c))
     _call("fg_dispatch", dev, rows, _TYPES[x.dtype], t, c, stride, at, k, out.shape[0], to, to_stride)
     return out

@@ -102,6 +102,12 @@ def test_combine_backward(lib):
     assert call(t=0, n=0) == call(t=0, order=None, bounds=None) == B.FG_OK
 
 
+def test_sizes_of_types_that_there_are_not():
+    for size in (lambda: B.fg_lookup_backward_workspace_size(5, 5, 5, torch.float64), lambda: B.fg_combine_backward_workspace_size(5, 5, 5, 5, torch.int32)):
+        with pytest.raises(B.FgError):
+            size()
+
+
 def test_the_binding_refuses_tensors_that_are_not_on_a_device():
     i, x = torch.zeros((4, 2), dtype=torch.int32), torch.zeros((4, 8))
     by = B.IndexSort(i, 4, torch.zeros(8 + 5 + 8, dtype=torch.int32), True)
