@@ -502,20 +502,21 @@ class IndexSort:
     def __init__(self, index: torch.Tensor, n_rows: int, words: torch.Tensor, place: bool):
         self.index, self.n_rows, self._words, self._place, self._views = index, n_rows, words, place, {}
 
-    def _view(self, name: str, first: int, count: int):
+    def _view(self, name: str):
         if name not in self._views:
-            self._views[name] = self._words[first:first + count]
+            m = self.index.numel()
+            self._views["order"], self._views["bounds"] = self._words.split_with_sizes((m, self.n_rows + 1, m) if self._place else (m, self.n_rows + 1))[:2]
         return self._views[name]
 
     @property
     def order(self) -> torch.Tensor:
         """[m] entries by row, ascending inside a row; those that name no row last."""
-        return self._view("order", 0, self.index.numel())
+        return self._view("order")
 
     @property
     def bounds(self) -> torch.Tensor:
         """[n_rows + 1] positions of the rows."""
-        return self._view("bounds", self.index.numel(), self.n_rows + 1)
+        return self._view("bounds")
 
     @property
     def place(self) -> torch.Tensor | None:

@@ -5,10 +5,10 @@
 // 64 entries at a time a wavefront finds, with one ballot for every bit of the digit, which lanes have the same digit; the number of
 // those before a lane is its rank, their count moves the wavefront's counter of that digit.
 //
-// A few entries are not sorted but counted: k_sort_few.  Up to 8192 one workgroup sorts in LDS, all digits in one launch.  Beyond, three launches a
-// digit (counts of the tiles, their prefix, the entries to their places) and one for the bounds: 262144 entries of 64 rows 15 us, 65536 of 131072 30
-// (latency: a tile's chain of loads, ranks and stores is 5 to 7 us, however few there are), 4M of 100k 82, 32M of 1M 720.  A pass over 4M moves 48 to 64 MB
-// in 23 to 26 us: stores of runs of 8 entries.
+// A few entries are not sorted but counted: k_sort_few.  Up to 8192 of many rows one workgroup sorts in LDS, all digits in one launch.  Beyond, three
+// launches a digit (counts of the tiles, their prefix, the entries to their places; where there are few counts, the last alone after the first digit's counts)
+// and one for the bounds: 262144 entries of 64 rows 12 us, 65536 of 131072 31 (latency: a tile's chain of loads, ranks and stores is 5 to 7 us, however few
+// there are), 4M of 100k 82, 32M of 1M 720.  A pass over 4M moves 48 to 64 MB in 23 to 26 us: stores of runs of 8 entries.
 #include "fg_rows.hpp"
 
 namespace fg {
@@ -17,10 +17,11 @@ namespace {
 
 constexpr int kMaxBits = 10;                 // of a digit: a million rows in two passes
 constexpr int kSmallBlock = 1024;
-// Entries that one workgroup sorts in LDS (8192 of 50000 rows 18 us, with the launches for more 27)
+// Entries that one workgroup sorts in LDS, where a row has two digits or more (8192 of 60000 rows 22 us in one launch, 20 in the four for more; with one
+// digit, 8192 of 256 rows, 14.6 and 7.9 in two).
 constexpr int64_t kSmallM = 8192;
-// Entries that are counted, by 4 and by 16 lanes a question, and how many questions (entries and bounds) and looks at a key at most.  us counted by 4 / counted by 16 / sorted
-// in LDS: 64 entries of 8 rows 1.7 / 2.1 / 3.0, 300 of 50000 4.2 / 5.3 / 7.0, 100 of 200000 5.5 / 8.6 / 7.9, 1000 of 5003 7.2 / 4.0 / 7.2, 1024 of 20000
+// Entries that are counted, by 4 and by 16 lanes a question, and how many questions (entries and bounds) and looks at a key at most.  us counted by 4 /
+// counted by 16 / sorted in LDS: 64 entries of 8 rows 1.7 / 2.1 / 3.0, 300 of 50000 4.2 / 5.3 / 7.0, 100 of 200000 5.5 / 8.6 / 7.9, 1000 of 5003 7.2 / 4.0 / 7.2, 1024 of 20000
 // 7.2 / 5.5 / 7.5, 1000 of 60000 7.7 / 8.3 / 7.6, 4096 of 10000 21 / 8.4 / 12.4, of 16000 21 / 12.0 / 12.5.  (8192 of 256 by 16 13.1, in LDS 14.6.)
 constexpr int64_t kFewM = 512, kFewQuestions = 1 << 18, kSomeM = 4096, kSomeQuestions = 1 << 15, kSomeLooks = 1 << 26;
 // Rows whose bounds a workgroup writes; for more, more workgroups sort the same entries (1000 entries of 5003 rows, before they were
@@ -33,8 +34,14 @@ constexpr unsigned kXcds = 8;
 constexpr int kItems = 4;
 constexpr int64_t kMediumM = 1 << 20;
 constexpr int kLargeBlock = 512, kLargeItems = 8;
+// Counts of a pass (tiles x digits) up to which every tile adds them up for itself and counts the next pass's digits as it goes, so that the launches
+// between two passes are saved (us with them / without, by tiles of as many entries, also where rows follow Zipf's law: 8200 entries of 5000 rows 26 / 19,
+// 32768 of 131072 31 / 24, 65536 of 64 11.2 / 8.5, 131072 of 2000 31 / 24; 65536 of 131072, 2^15 counts, 32 / 30; 131072 of 131072, 2^16, 35 / 41).
+constexpr int kJoinedBits = 15;
+constexpr int64_t kJoinedCounts = 1 << kJoinedBits;
+constexpr int kJoinedBlock = kBlock * kItems;
 
-struct Plan { int bits, passes; bool large; int64_t tiles; };
+struct Plan { int bits, passes; bool joined, large; int64_t tiles; };
 
 inline Plan plan_for(int64_t m, int64_t n_rows)
 {
@@ -46,6 +53,7 @@ inline Plan plan_for(int64_t m, int64_t n_rows)
     p.large = m > kMediumM;
     const int64_t tile = p.large ? kLargeBlock * kLargeItems : kBlock * kItems;
     p.tiles = (m + tile - 1) / tile;
+    p.joined = !p.large && p.tiles << p.bits <= kJoinedCounts;
     return p;
 }
 
@@ -58,7 +66,7 @@ inline Layout layout_for(int64_t m, const Plan& p)
     Layout l;
     const size_t words = up((size_t)m * 4);
     l.counts = 0;
-    l.totals = up(((size_t)1 << p.bits) * (size_t)p.tiles * 4);
+    l.totals = up(((size_t)1 << p.bits) * (size_t)p.tiles * 4) * (p.joined ? p.passes : 1);       // (joined: of every pass)
     l.key_a = l.totals + up(((size_t)1 << p.bits) * 4);
     l.order_a = l.key_a + (p.passes > 1 ? words : 0);
     l.key_b = l.order_a + (p.passes > 1 ? words : 0);
@@ -69,7 +77,7 @@ inline Layout layout_for(int64_t m, const Plan& p)
 
 inline bool takes_few(int64_t m, int64_t n_rows) { return m <= kFewM && m + n_rows < kFewQuestions; }
 inline bool takes_some(int64_t m, int64_t n_rows) { return m <= kSomeM && m + n_rows < kSomeQuestions && m * (m + n_rows) < kSomeLooks; }
-inline bool takes_small_sort(int64_t m) { return m <= kSmallM; }
+inline bool takes_small_sort(int64_t m, const Plan& p) { return m <= kSmallM && p.passes > 1; }
 
 __device__ __forceinline__ uint32_t key_of(int32_t name, uint32_t n_rows) { return (uint32_t)name < n_rows ? (uint32_t)name : n_rows; }
 
@@ -278,9 +286,10 @@ __global__ __launch_bounds__(kBlock) void k_sort_bounds(const uint32_t* __restri
 
 // ---- many workgroups, one digit a pass ---------------------------------------------------------------------------------
 
-template <int BLOCK, int ITEMS>
+// JOIN: the counts of a tile lie together, and those of the `later` passes, `later_counts` words on each, which k_sort_scatter makes, begin at zero.
+template <int BLOCK, int ITEMS, bool JOIN>
 __global__ __launch_bounds__(BLOCK) void k_sort_count(const uint32_t* __restrict__ keys, int64_t m, uint32_t n_rows, int shift, int bits, int64_t tiles,
-                                                      uint32_t* __restrict__ counts)
+                                                      uint32_t* __restrict__ counts, int64_t later_counts, int later)
 {
     typedef uint32_t Four __attribute__((ext_vector_type(4), aligned(4)));
     __shared__ uint32_t counter[1 << kMaxBits];
@@ -291,8 +300,9 @@ __global__ __launch_bounds__(BLOCK) void k_sort_count(const uint32_t* __restrict
     __syncthreads();
     const int64_t first = tile * (BLOCK * ITEMS);
     auto add = [&](uint32_t key) { atomicAdd(&counter[(key_of((int32_t)key, n_rows) >> shift) & (digits - 1)], 1u); };
-    if (first + BLOCK * ITEMS <= m) {
-        Four v[ITEMS / 4];
+    const int64_t end = first + BLOCK * ITEMS < m ? first + BLOCK * ITEMS : m;
+    if (ITEMS >= 4 && first + BLOCK * ITEMS <= m) {
+        Four v[ITEMS < 4 ? 1 : ITEMS / 4];
 #pragma unroll
         for (int i = 0; i < ITEMS / 4; ++i) v[i] = *reinterpret_cast<const Four*>(keys + first + (i * BLOCK + threadIdx.x) * 4);
 #pragma unroll
@@ -300,10 +310,14 @@ __global__ __launch_bounds__(BLOCK) void k_sort_count(const uint32_t* __restrict
 #pragma unroll
             for (int j = 0; j < 4; ++j) add(v[i][j]);
     } else {
-        for (int64_t e = first + threadIdx.x; e < m; e += BLOCK) add(keys[e]);
+        for (int64_t e = first + threadIdx.x; e < end; e += BLOCK) add(keys[e]);
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < digits; d += BLOCK) counts[(int64_t)d * tiles + tile] = counter[d];
+    for (int d = threadIdx.x; d < digits; d += BLOCK) {
+        counts[JOIN ? tile * digits + d : (int64_t)d * tiles + tile] = counter[d];
+        if (JOIN)
+            for (int p = 1; p <= later; ++p) counts[p * later_counts + tile * digits + d] = 0;
+    }
 }
 
 // One workgroup a digit: exclusive prefix over the tiles, and the sum.
@@ -330,14 +344,16 @@ __global__ __launch_bounds__(kBlock) void k_sort_scan(uint32_t* __restrict__ cou
 // A tile is put in order in LDS first, so that its entries of one digit leave as one run; runs of neighbouring tiles lie next to each other.  (4M
 // entries: every lane storing its own 75 us a pass, runs 38, with more wavefronts a workgroup 25.)
 // FIRST: keys are the index itself and entries are numbered as they come.  LAST: place is written, with one pass in all the bounds too.
-template <int BLOCK, int ITEMS>
-constexpr size_t scatter_lds(int digits) { return ((size_t)digits * (BLOCK / 64 + 1) + 2 * BLOCK * ITEMS) * 4; }
+// JOIN: counts [tile][digit] are added up here, and those of the pass that follows made (`next`).
+template <int BLOCK, int ITEMS, bool JOIN>
+constexpr size_t scatter_lds(int digits) { return ((size_t)digits * (BLOCK / 64 + (JOIN ? 3 : 1)) + 2 * BLOCK * ITEMS) * 4; }
 
-template <int BLOCK, int ITEMS, bool FIRST, bool LAST>
+template <int BLOCK, int ITEMS, bool JOIN, bool FIRST, bool LAST>
 __global__ __launch_bounds__(BLOCK) void k_sort_scatter(const uint32_t* __restrict__ keys, const int32_t* __restrict__ from, int64_t m, uint32_t n_rows,
                                                         int shift, int bits, int64_t tiles, const uint32_t* __restrict__ counts,
                                                         const uint32_t* __restrict__ totals, uint32_t* __restrict__ keys_out,
-                                                        int32_t* __restrict__ order, int32_t* __restrict__ place, int32_t* __restrict__ bounds)
+                                                        int32_t* __restrict__ order, int32_t* __restrict__ place, int32_t* __restrict__ bounds,
+                                                        uint32_t* __restrict__ next)
 {
     constexpr int kTile = BLOCK * ITEMS, kWaves = BLOCK / 64, kOwn = (1 << kMaxBits) / BLOCK;
     extern __shared__ uint32_t lds[];                    // scatter_lds()
@@ -361,11 +377,32 @@ __global__ __launch_bounds__(BLOCK) void k_sort_scatter(const uint32_t* __restri
         entry[i] = FIRST || e >= m ? (int32_t)e : from[e];
     }
     uint32_t total[kOwn], already[kOwn];                 // of this lane's digits: in the index, in the tiles before
+    uint32_t* joined = counters + kWaves * digits;       // JOIN: [digit] total, [digit] already
+    if constexpr (JOIN) {
+        static_assert(kOwn == 1, "a lane has one digit at most");
+        if (tid < digits) joined[tid] = joined[digits + tid] = 0;
+        __syncthreads();
+        const int groups = BLOCK >> bits, d = tid & (digits - 1);
+        uint32_t sum = 0, sum_before = 0;
+        for (int t0 = tid >> bits; t0 < tiles; t0 += groups * 8) {
+            uint32_t n[8];
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-        const int d = i * BLOCK + tid;
-        total[i] = d < digits ? totals[d] : 0;
-        already[i] = d < digits ? counts[(int64_t)d * tiles + tile] : 0;
+            for (int u = 0; u < 8; ++u) n[u] = counts[(t0 + u * groups < tiles ? t0 + u * groups : 0) * digits + d];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                sum += t0 + u * groups < tiles ? n[u] : 0;
+                sum_before += t0 + u * groups < tile ? n[u] : 0;
+            }
+        }
+        if (sum) atomicAdd(&joined[d], sum);
+        if (sum_before) atomicAdd(&joined[digits + d], sum_before);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            const int d = i * BLOCK + tid;
+            total[i] = d < digits ? totals[d] : 0;
+            already[i] = d < digits ? counts[(int64_t)d * tiles + tile] : 0;
+        }
     }
     for (int d = lane; d < digits; d += 64) counter[d] = 0;
     __builtin_amdgcn_wave_barrier();
@@ -373,6 +410,10 @@ __global__ __launch_bounds__(BLOCK) void k_sort_scatter(const uint32_t* __restri
     for (int i = 0; i < ITEMS; ++i)
         rank[i] = rank_in_wave(counter, (key[i] >> shift) & (digits - 1), bits, first + i * 64 + lane < m);
     __syncthreads();
+    if constexpr (JOIN) {
+        total[0] = tid < digits ? joined[tid] : 0;
+        already[0] = tid < digits ? joined[digits + tid] : 0;
+    }
     uint64_t before = 0;                                 // of the whole order in the upper half, of the tile in the lower
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
@@ -416,22 +457,28 @@ __global__ __launch_bounds__(BLOCK) void k_sort_scatter(const uint32_t* __restri
             order[to] = entries[p];
             if (keys_out) keys_out[to] = k;
             if (LAST && place) place[entries[p]] = k < n_rows ? (int32_t)to : -1;
+            if (JOIN && !LAST) {
+                // (one addition for the entries of a wavefront that are counted together: those of a row that is named often)
+                const uint32_t at = (to / kTile) * digits + ((k >> (shift + bits)) & (digits - 1));
+                const uint64_t peers = same_digit(at, kJoinedBits, true);
+                if ((peers & ((1ull << lane) - 1)) == 0) atomicAdd(&next[at], (uint32_t)__popcll(peers));
+            }
         }
     }
 }
 
-template <int BLOCK, int ITEMS, bool FIRST, bool LAST, typename... Args>
+template <int BLOCK, int ITEMS, bool JOIN, bool FIRST, bool LAST, typename... Args>
 hipError_t scatter(unsigned blocks, int bits, hipStream_t stream, Args... args)
 {
-    const size_t lds = scatter_lds<BLOCK, ITEMS>(1 << bits);
+    const size_t lds = scatter_lds<BLOCK, ITEMS, JOIN>(1 << bits);
     // (beyond 64 KiB a kernel has to be told)
     if (lds > 65536)
-        FG_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_sort_scatter<BLOCK, ITEMS, FIRST, LAST>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    FG_LAUNCH((k_sort_scatter<BLOCK, ITEMS, FIRST, LAST>), dim3(blocks), dim3(BLOCK), lds, stream, args...);
+        FG_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_sort_scatter<BLOCK, ITEMS, JOIN, FIRST, LAST>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    FG_LAUNCH((k_sort_scatter<BLOCK, ITEMS, JOIN, FIRST, LAST>), dim3(blocks), dim3(BLOCK), lds, stream, args...);
     return hipSuccess;
 }
 
-template <int BLOCK, int ITEMS>
+template <int BLOCK, int ITEMS, bool JOIN>
 hipError_t many(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, int32_t* order, int32_t* place, int32_t* bounds, char* ws,
                 hipStream_t stream)
 {
@@ -442,17 +489,21 @@ hipError_t many(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, 
     const uint32_t* keys = (const uint32_t*)index;
     const int32_t* from = nullptr;
     const unsigned spread = (unsigned)((p.tiles + kXcds - 1) / kXcds * kXcds);
+    const int64_t later_counts = (int64_t)(l.totals / p.passes / sizeof(uint32_t));      // (joined)
     for (int pass = 0; pass < p.passes; ++pass) {
         const bool first = pass == 0, last = pass == p.passes - 1;
         const int shift = pass * p.bits;
         uint32_t* keys_out = p.passes > 1 ? key_to[pass & 1] : nullptr;
         int32_t* out = last ? order : order_to[pass & 1];
         int32_t* starts = p.passes == 1 ? bounds : nullptr;
-        FG_LAUNCH((k_sort_count<BLOCK, ITEMS>), dim3(spread), dim3(BLOCK), 0, stream, keys, m, (uint32_t)n_rows, shift, p.bits, p.tiles, counts);
-        FG_LAUNCH(k_sort_scan, dim3(1u << p.bits), dim3(kBlock), 0, stream, counts, p.tiles, totals);
+        if (first || !JOIN)
+            FG_LAUNCH((k_sort_count<BLOCK, ITEMS, JOIN>), dim3(spread), dim3(BLOCK), 0, stream, keys, m, (uint32_t)n_rows, shift, p.bits, p.tiles, counts,
+                      later_counts, p.passes - 1);
+        if (!JOIN) FG_LAUNCH(k_sort_scan, dim3(1u << p.bits), dim3(kBlock), 0, stream, counts, p.tiles, totals);
 #define FG_SCATTER(FIRST, LAST)                                                                                                          \
-    FG_TRY((scatter<BLOCK, ITEMS, FIRST, LAST>(spread, p.bits, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,          \
-                                               (const uint32_t*)counts, (const uint32_t*)totals, keys_out, out, place, starts)))
+    FG_TRY((scatter<BLOCK, ITEMS, JOIN, FIRST, LAST>(spread, p.bits, stream, keys, from, m, (uint32_t)n_rows, shift, p.bits, p.tiles,    \
+                                                     (const uint32_t*)counts, (const uint32_t*)totals, keys_out, out, place, starts,     \
+                                                     JOIN ? counts + later_counts : nullptr)))
         if (first && last) FG_SCATTER(true, true);
         else if (first) FG_SCATTER(true, false);
         else if (last) FG_SCATTER(false, true);
@@ -460,6 +511,7 @@ hipError_t many(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p, 
 #undef FG_SCATTER
         keys = keys_out;
         from = out;
+        if (JOIN) counts += later_counts;
     }
     if (p.passes > 1)
         FG_LAUNCH(k_sort_bounds, dim3((unsigned)(n_rows / kBlock + 1)), dim3(kBlock), 0, stream, keys, (int32_t)m, n_rows, bounds);
@@ -479,8 +531,8 @@ hipError_t small(const int32_t* index, int64_t m, int64_t n_rows, const Plan& p,
 
 size_t index_sort_workspace_bytes(int64_t m, int64_t n_rows)
 {
-    if (takes_small_sort(m)) return 0;
-    return layout_for(m, plan_for(m, n_rows)).total;
+    const Plan p = plan_for(m, n_rows);
+    return takes_few(m, n_rows) || takes_some(m, n_rows) || takes_small_sort(m, p) ? 0 : layout_for(m, p).total;
 }
 
 hipError_t launch_index_sort(const int32_t* index, int64_t m, int64_t n_rows, int32_t* order, int32_t* place, int32_t* bounds, void* workspace,
@@ -489,13 +541,14 @@ hipError_t launch_index_sort(const int32_t* index, int64_t m, int64_t n_rows, in
     const Plan p = plan_for(m, n_rows);
     if (takes_few(m, n_rows)) return count_few<4>(index, m, n_rows, order, place, bounds, stream);
     if (takes_some(m, n_rows)) return count_few<16>(index, m, n_rows, order, place, bounds, stream);
-    if (takes_small_sort(m)) {
+    if (takes_small_sort(m, p)) {
         if (m <= kSmallBlock) return small<1>(index, m, n_rows, p, order, place, bounds, stream);
         if (m <= 4 * kSmallBlock) return small<4>(index, m, n_rows, p, order, place, bounds, stream);
         return small<8>(index, m, n_rows, p, order, place, bounds, stream);
     }
-    if (!p.large) return many<kBlock, kItems>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);
-    return many<kLargeBlock, kLargeItems>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);
+    if (p.joined) return many<kJoinedBlock, 1, true>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);
+    if (!p.large) return many<kBlock, kItems, false>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);
+    return many<kLargeBlock, kLargeItems, false>(index, m, n_rows, p, order, place, bounds, (char*)workspace, stream);
 }
 
 }  // namespace fg

@@ -60,11 +60,14 @@ CHAINS = {
     "some entries, still more rows": (("sort", dict(m=1024, n=(1 << 15) - 1024)), ["k_sort_small"]),
     "some entries of more rows": (("sort", dict(m=4096, n=(1 << 14) - 4096)), ["k_sort_small"]),
     "entries that one workgroup sorts": (("sort", dict(m=8192, n=100000)), ["k_sort_small"]),
-    "one digit": (("sort", dict(m=8193, n=1023)), PASS),
-    "two digits": (("sort", dict(m=100000, n=1024)), PASS * 2 + ["k_sort_bounds"]),
+    "one digit, few counts": (("sort", dict(m=4097, n=1023)), ["k_sort_count", "k_sort_scatter"]),
+    "one digit": (("sort", dict(m=8193 * 4, n=1023)), PASS),
+    "two digits, few counts": (("sort", dict(m=65536, n=131072)), ["k_sort_count"] + ["k_sort_scatter"] * 2 + ["k_sort_bounds"]),
+    "four digits, few counts": (("sort", dict(m=20000, n=1 << 30)), ["k_sort_count"] + ["k_sort_scatter"] * 4 + ["k_sort_bounds"]),
+    "two digits": (("sort", dict(m=65537, n=131072)), PASS * 2 + ["k_sort_bounds"]),
     "two digits, many entries": (("sort", dict(m=1 << 21, n=(1 << 20) - 1)), PASS * 2 + ["k_sort_bounds"]),
-    "three digits": (("sort", dict(m=100000, n=1 << 20)), PASS * 3 + ["k_sort_bounds"]),
-    "four digits": (("sort", dict(m=100000, n=1 << 30)), PASS * 4 + ["k_sort_bounds"]),
+    "three digits": (("sort", dict(m=500000, n=1 << 20)), PASS * 3 + ["k_sort_bounds"]),
+    "four digits": (("sort", dict(m=500000, n=1 << 30)), PASS * 4 + ["k_sort_bounds"]),
     "lookup": (("lookup", dict(type=BF16, n=1000, c=1024, m=500)), ["k_lookup"]),
     "lookup, narrow rows": (("lookup", dict(type=BF16, n=1000, c=7, m=500)), ["k_lookup"]),
     "lookup, past the caches": (("lookup", dict(type=BF16, n=1000, c=2048, m=1 << 17)), ["k_lookup"]),
