@@ -5,7 +5,8 @@
  * partitioned into a regular grid of bins, sorted by bin, and every point searches shells of
  * neighbouring bins of growing radius until its K best squared distances are certified
  * against everything unsearched (Algorithm 1, Algorithm 2); gradients of the returned squared
- * distances flow back to the coordinates (Section 3, last paragraph).
+ * distances flow back to the coordinates (Section 3, last paragraph).  "Rows by index", at the end,
+ * is what a network does with such an index: lookups and weighted sums of rows, with their gradients.
  *
  * Conventions for every entry point
  *   - Every array pointer is a DEVICE pointer unless the comment says "host".

@@ -1,4 +1,5 @@
-"""MI355X-native binned exact k-nearest-neighbour graph build (FastGraph, Section 3).
+"""MI355X-native binned exact k-nearest-neighbour graph build (FastGraph, Section 3), and rows by index: lookups, sums over
+neighbours, tokens to experts and back, with their gradients.
 
 The package holds the HIP kernels + C-ABI library (``csrc/``), a thin ctypes
 binding with the same names (``binding``) and the seeded input generators
