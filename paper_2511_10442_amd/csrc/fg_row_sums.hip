@@ -126,7 +126,7 @@ __device__ __forceinline__ void within(const SumArgs& a, int32_t& from, int32_t&
 __device__ __forceinline__ int32_t first_chunk(const SumArgs& a, int32_t from) { return (int32_t)(((int64_t)from + (1 << a.shift) - 1) >> a.shift); }
 
 template <typename T, int N, typename TO, bool ACCUMULATE, bool STREAM, int S>
-__device__ __forceinline__ void store_sum(const SumArgs& a, typename Piece<T, N>::Wide (&sum)[S], TO* __restrict__ out, int64_t out_stride, int64_t row,
+__device__ __forceinline__ void store_sum(float scale, typename Piece<T, N>::Wide (&sum)[S], TO* __restrict__ out, int64_t out_stride, int64_t row,
                                           const Span<S>& at)
 {
     typedef TO OutVec __attribute__((ext_vector_type(N), aligned(sizeof(TO))));
@@ -135,7 +135,7 @@ __device__ __forceinline__ void store_sum(const SumArgs& a, typename Piece<T, N>
     for (int s = 0; s < S; ++s) {
         if (!at.there[s] || at.skip[s] >= N) continue;
         TO* p = out + row * out_stride + at.col[s];
-        Wide x = sum[s] * a.scale;
+        Wide x = sum[s] * scale;
         if (!ACCUMULATE || at.skip[s] == 0) {
             if (ACCUMULATE) x += __builtin_convertvector(*reinterpret_cast<const OutVec*>(p), Wide);
             store_vec<STREAM>(p, __builtin_convertvector(x, OutVec));
@@ -198,7 +198,8 @@ __global__ __launch_bounds__(kBlock, DOTS && sizeof(T) == 2 ? 3 : 4) void k_row_
             for (int s = 0; s < S; ++s)
                 if (real && at.there[s]) *reinterpret_cast<typename P::Wide*>(a.parts + (at.row * d.pieces + at.piece[s]) * N) = sum[s];
         } else {
-            store_sum<T, N, TO, ACCUMULATE, STREAM, S>(a, sum, out, out_stride, name, at);
+            // (no entries: zeros, whatever the scale)
+            store_sum<T, N, TO, ACCUMULATE, STREAM, S>(from < to ? a.scale : 0.0f, sum, out, out_stride, name, at);
         }
     });
 }
@@ -239,7 +240,7 @@ __global__ __launch_bounds__(kFewBlock) void k_row_sums_few(SumArgs a, const int
     if (there && to - from <= kAlone && !(ACCUMULATE && from >= to)) {
         Wide sum[1] = {}, none = {};
         add_entries<T, N, WEIGHTED, false, 1>(sum, a, grad, grad_stride, from, to, at, none, true, 0);
-        store_sum<T, N, TO, ACCUMULATE, false, 1>(a, sum, out, out_stride, row, at);
+        store_sum<T, N, TO, ACCUMULATE, false, 1>(from < to ? a.scale : 0.0f, sum, out, out_stride, row, at);
     }
     __syncthreads();
     for (int w = 0; w < kW; ++w) {
@@ -256,7 +257,7 @@ __global__ __launch_bounds__(kFewBlock) void k_row_sums_few(SumArgs a, const int
             sum[0] = part[0][lane];
 #pragma unroll
             for (int i = 1; i < kW; ++i) sum[0] += part[i][lane];
-            store_sum<T, N, TO, ACCUMULATE, false, 1>(a, sum, out, out_stride, row, at);
+            store_sum<T, N, TO, ACCUMULATE, false, 1>(a.scale, sum, out, out_stride, row, at);
         }
         __syncthreads();
     }
@@ -304,7 +305,7 @@ __global__ __launch_bounds__(kBlock) void k_row_join(SumArgs a, TO* __restrict__
         } else {
             add_parts<T, N>(sum[0], parts, stride, q0, q1);
         }
-        store_sum<T, N, TO, ACCUMULATE, false, 1>(a, sum, out, out_stride, name, at);
+        store_sum<T, N, TO, ACCUMULATE, false, 1>(a.scale, sum, out, out_stride, name, at);
     });
 }
 

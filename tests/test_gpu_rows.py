@@ -227,6 +227,20 @@ def test_a_row_of_five_million_entries():
     R.check(got, ref, mass, 5000, torch.float32)
 
 
+@pytest.mark.parametrize("m,n_rows,c", [(20, 40, 64), (5000, 9000, 33), (5000, 9000, 1024)])
+@pytest.mark.parametrize("scale", [float("inf"), float("nan")])
+def test_a_scale_that_is_not_finite_leaves_rows_without_entries_zero(m, n_rows, c, scale):
+    index = dev(np.arange(m, dtype=np.int32) * 2 % n_rows // 4)
+    grad = torch.ones((m, c), device=DEV)
+    got = B.fg_lookup_backward(grad, B.fg_index_sort(index, n_rows), scale)
+    named = torch.zeros(n_rows, dtype=torch.bool, device=DEV)
+    named[index.long()] = True
+    assert bool((got[~named] == 0).all()) and not bool(torch.isfinite(got[named]).any())
+    index[::3] = -1
+    got = B.fg_lookup(grad, index, scale)
+    assert bool((got[index < 0] == 0).all()) and not bool(torch.isfinite(got[(index >= 0) & (index < m)]).any())
+
+
 def test_what_is_not_finite_stays_in_its_row():
     rng = np.random.default_rng(6)
     index = some_index(rng, (400,), 20)
