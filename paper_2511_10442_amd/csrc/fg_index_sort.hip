@@ -34,11 +34,12 @@ constexpr unsigned kXcds = 8;
 constexpr int kItems = 4;
 constexpr int64_t kMediumM = 1 << 20;
 constexpr int kLargeBlock = 512, kLargeItems = 8;
-// Counts of a pass (tiles x digits) up to which every tile adds them up for itself and counts the next pass's digits as it goes, so that the launches
+// Tiles and counts of a pass (tiles x digits) up to which every tile adds them up for itself and counts the next pass's digits as it goes, so that the launches
 // between two passes are saved (us with them / without, by tiles of as many entries, also where rows follow Zipf's law: 8200 entries of 5000 rows 26 / 19,
-// 32768 of 131072 31 / 24, 65536 of 64 11.2 / 8.5, 131072 of 2000 31 / 24; 65536 of 131072, 2^15 counts, 32 / 30; 131072 of 131072, 2^16, 35 / 41).
+// 32768 of 131072 31 / 24, 65536 of 64 11.2 / 8.5, 131072 of 2000 31 / 24; 65536 of 131072, 2^15 counts, 32 / 30; 131072 of 131072, 2^16, 35 / 41;
+// 196 tiles, 200000 entries of 8 rows, 11.1 / 8.8, 489, 500000 of 16, 13.5 / 15.2).
 constexpr int kJoinedBits = 15;
-constexpr int64_t kJoinedCounts = 1 << kJoinedBits;
+constexpr int64_t kJoinedCounts = 1 << kJoinedBits, kJoinedTiles = 256;
 constexpr int kJoinedBlock = kBlock * kItems;
 
 struct Plan { int bits, passes; bool joined, large; int64_t tiles; };
@@ -53,7 +54,7 @@ inline Plan plan_for(int64_t m, int64_t n_rows)
     p.large = m > kMediumM;
     const int64_t tile = p.large ? kLargeBlock * kLargeItems : kBlock * kItems;
     p.tiles = (m + tile - 1) / tile;
-    p.joined = !p.large && p.tiles << p.bits <= kJoinedCounts;
+    p.joined = !p.large && p.tiles <= kJoinedTiles && p.tiles << p.bits <= kJoinedCounts;
     return p;
 }
 

@@ -57,7 +57,7 @@ def test_sort(m, n_rows):
 
 
 @pytest.mark.parametrize("m,n_rows", [(1048576, 300), (1048577, 300), (1200003, 100003), (30000, 1048575), (30000, 1048576), (1300000, 1300000),
-                                      (32768, 1023), (32769, 1023), (65536, 131072), (65537, 131072), (131072, 2047), (262144, 127), (262145, 127), (700000, 40000)])
+                                      (32768, 1023), (32769, 1023), (65536, 131072), (65537, 131072), (131072, 2047), (262144, 127), (262145, 127), (262145, 8), (700000, 40000)])
 def test_sort_many(m, n_rows):
     rng = np.random.default_rng(m)
     check_sort(some_index(rng, (m,), n_rows, "frequent"), n_rows)

@@ -61,6 +61,8 @@ CHAINS = {
     "some entries of more rows": (("sort", dict(m=4096, n=(1 << 14) - 4096)), ["k_sort_small"]),
     "entries that one workgroup sorts": (("sort", dict(m=8192, n=100000)), ["k_sort_small"]),
     "one digit, few counts": (("sort", dict(m=4097, n=1023)), ["k_sort_count", "k_sort_scatter"]),
+    "one digit, few tiles": (("sort", dict(m=262144, n=8)), ["k_sort_count", "k_sort_scatter"]),
+    "one digit, more tiles": (("sort", dict(m=262145, n=8)), PASS),
     "one digit": (("sort", dict(m=8193 * 4, n=1023)), PASS),
     "two digits, few counts": (("sort", dict(m=65536, n=131072)), ["k_sort_count"] + ["k_sort_scatter"] * 2 + ["k_sort_bounds"]),
     "four digits, few counts": (("sort", dict(m=20000, n=1 << 30)), ["k_sort_count"] + ["k_sort_scatter"] * 4 + ["k_sort_bounds"]),
