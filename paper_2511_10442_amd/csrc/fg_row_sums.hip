@@ -13,7 +13,7 @@ namespace {
 // graph are all named often, and as chunks they would be read by a few scattered lanes: there it grows to four times the mean of a row's
 // entries, as far as the rows alone give 512 lanes for every entry of a chunk, so that one lane's share stays small beside the whole (a power of two;
 // 20k points, 40 neighbours of 64 float32: 57 us with chunks of 32, 42 with 256; 9k points, 100 neighbours of 128 78 and 50; but entries whose rows follow
-// Zipf's law, 1M of 5000 rows of 64 bf16, 308 us with 64 lanes, 90 with 256, 62 so; 66k of 105 rows of 2112 147, 90, 80).
+// Zipf's law, 1M of 5000 rows of 64 bf16, 308 us with 64 lanes, 90 with 256, 62 so, by now 55; 66k of 105 rows of 2112 147, 90, 80).
 //   k_row_sums   chunks of one row each, a row's first and last with its entries before and after them: their sums; rows without such a chunk
 //   k_row_parts  chunks of chunks (where there are enough entries)
 //   k_row_join   rows with a chunk: chunks up to the first whole chunk of chunks, those, and chunks again
