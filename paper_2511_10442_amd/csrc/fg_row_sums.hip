@@ -205,7 +205,8 @@ __global__ __launch_bounds__(kBlock, DOTS && sizeof(T) == 2 ? 3 : 4) void k_row_
         }
         const bool real = !DOTS || at.skip[0] < N;
         typename P::Wide sum[S] = {}, row = {};
-        if (DOTS && from < to) row = wide<T, N>(load_piece<T, N>(rows + name * rows_stride + at.col[0]));
+        // (a lane without a piece has zeros of the row too: it would add zero times the row's last piece, infinities and all)
+        if (DOTS && from < to) row = wide<T, N>(only_if<T, N>(real, load_piece<T, N>(rows + name * rows_stride + at.col[0])));
         add_entries<T, N, WEIGHTED, DOTS, !DOTS && !STREAM, S>(sum, a, grad, grad_stride, from, to, at, row, real, (int)d.pieces);
         if (chunk) {
 #pragma unroll
