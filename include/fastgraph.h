@@ -264,7 +264,7 @@ fg_status fg_oc_helper(const int32_t* asso_idx, const int32_t* unique_idx, const
  * Outputs must not overlap inputs.
  *   1 <= c <= FG_MAX_C, strides <= FG_MAX_STRIDE, 1 <= k <= FG_MAX_K; rows, index entries (t * k) <= FG_MAX_N
  * Errors besides those of the other calls: FG_ERR_UNSUPPORTED for an unknown type or a pointer that an element of its type
- * may not have.  The sorted form of an index (order, bounds) must be fg_index_sort's of that index with that n_rows. */
+ * may not have (rows, weights, and the int32 of an index, its order and bounds).  The sorted form of an index (order, bounds) must be fg_index_sort's of that index with that n_rows. */
 typedef enum {
     FG_F32 = 0,
     FG_BF16 = 1,

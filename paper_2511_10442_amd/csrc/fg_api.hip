@@ -536,6 +536,7 @@ static bool misaligned(int32_t type, std::initializer_list<const void*> rows)
         if ((uintptr_t)p % (uintptr_t)type_bytes(type) != 0) return true;
     return false;
 }
+static bool misaligned_words(std::initializer_list<const void*> words) { return misaligned(FG_F32, words); }      // int32 or float32
 static bool bad_workspace(const void* workspace, size_t have, size_t need)
 {
     return need != 0 && (!workspace || (uintptr_t)workspace % kAlign != 0 || have < need);
@@ -556,6 +557,7 @@ fg_status fg_index_sort(const int32_t* index, int64_t m, int64_t n_rows, int32_t
 {
     if (bad_count(m) || bad_count(n_rows)) return FG_ERR_BAD_SHAPE;
     if (!bounds || (m > 0 && (!index || !order))) return FG_ERR_NULL;
+    if (misaligned_words({index, order, place, bounds})) return FG_ERR_UNSUPPORTED;
     if (bad_workspace(workspace, workspace_bytes, index_sort_workspace_bytes(m, n_rows))) return FG_ERR_WORKSPACE;
     return told(launch_index_sort(index, m, n_rows, order, place, bounds, workspace, (hipStream_t)stream));
 }
@@ -568,7 +570,7 @@ fg_status fg_lookup(const void* table, int32_t type, int64_t n_rows, int64_t c, 
     if (bad_count(m) || bad_count(n_rows)) return FG_ERR_BAD_SHAPE;
     if (m == 0) return FG_OK;
     if (!index || !out || (!table && n_rows > 0)) return FG_ERR_NULL;
-    if (misaligned(type, {table, out})) return FG_ERR_UNSUPPORTED;
+    if (misaligned(type, {table, out}) || misaligned_words({index})) return FG_ERR_UNSUPPORTED;
     return told(launch_lookup(type, {table, table_stride}, n_rows, c, index, m, scale, {out, out_stride}, (hipStream_t)stream));
 }
 
@@ -593,7 +595,7 @@ fg_status fg_lookup_backward(const void* grad_out, int32_t type, int64_t m, int6
     if (bad_count(m) || bad_count(n_rows)) return FG_ERR_BAD_SHAPE;
     if (n_rows == 0) return FG_OK;
     if (!bounds || !grad_table || (m > 0 && (!grad_out || !index || !order))) return FG_ERR_NULL;
-    if (misaligned(type, {grad_out}) || misaligned(grad_type, {grad_table})) return FG_ERR_UNSUPPORTED;
+    if (misaligned(type, {grad_out}) || misaligned(grad_type, {grad_table}) || misaligned_words({index, order, bounds})) return FG_ERR_UNSUPPORTED;
     if (bad_workspace(workspace, workspace_bytes, row_sums_workspace_bytes(type, m, n_rows, c, false))) return FG_ERR_WORKSPACE;
     RowSums a = {};
     a.type = type; a.out_type = grad_type;
@@ -612,7 +614,7 @@ fg_status fg_dispatch(const void* x, int32_t type, int64_t t, int64_t c, int64_t
     if (bad_fan(t, k) || bad_count(n_rows)) return FG_ERR_BAD_SHAPE;
     if (t == 0 || n_rows == 0) return FG_OK;
     if (!x || !place || !out) return FG_ERR_NULL;
-    if (misaligned(type, {x, out})) return FG_ERR_UNSUPPORTED;
+    if (misaligned(type, {x, out}) || misaligned_words({place})) return FG_ERR_UNSUPPORTED;
     return told(launch_dispatch(type, {x, x_stride}, t, c, place, k, n_rows, {out, out_stride}, (hipStream_t)stream));
 }
 
@@ -624,7 +626,7 @@ fg_status fg_combine(const void* rows, int32_t type, int64_t n_rows, int64_t c, 
     if (bad_fan(t, k) || bad_count(n_rows)) return FG_ERR_BAD_SHAPE;
     if (t == 0) return FG_OK;
     if (!index || !out || (!rows && n_rows > 0)) return FG_ERR_NULL;
-    if (misaligned(type, {rows, out})) return FG_ERR_UNSUPPORTED;
+    if (misaligned(type, {rows, out}) || misaligned_words({index, weights, walk})) return FG_ERR_UNSUPPORTED;
     return told(launch_combine(type, {rows, rows_stride}, n_rows, c, index, weights, t, k, walk, {out, out_stride}, (hipStream_t)stream));
 }
 
@@ -652,7 +654,7 @@ fg_status fg_combine_backward(const void* grad_out, int32_t type, int64_t t, int
     const bool shared = order || bounds;
     if (t > 0 && (!grad_out || !index || (grad_weights && !rows && n_rows > 0))) return FG_ERR_NULL;
     if (shared && (!bounds || (t > 0 && !order))) return FG_ERR_NULL;
-    if (misaligned(type, {grad_out, rows, grad_rows})) return FG_ERR_UNSUPPORTED;
+    if (misaligned(type, {grad_out, rows, grad_rows}) || misaligned_words({index, weights, order, bounds, walk, grad_weights})) return FG_ERR_UNSUPPORTED;
     const bool sums = shared && grad_rows && n_rows > 0, products = sums && t > 0 && grad_weights && sums_with_products(type, c);
     if (sums && bad_workspace(workspace, workspace_bytes, row_sums_workspace_bytes(type, t * k, n_rows, c, products))) return FG_ERR_WORKSPACE;
     if (sums) {

@@ -115,3 +115,20 @@ def test_the_binding_refuses_tensors_that_are_not_on_a_device():
                  lambda: B.fg_dispatch(x, i), lambda: B.fg_combine(x, i), lambda: B.fg_combine_backward(x, x, i)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_pointers_that_int32_and_float32_may_not_have(lib):
+    """Indexes, orders, bounds and weights between two elements' places are refused as rows are"""
+    bad = lambda f, args, names: [n for n in names if f(*dict(args, **{n: args[n] + 2}).values(), None) != B.FG_ERR_UNSUPPORTED]      # noqa: E731
+    sort = dict(index=8, m=100000, n=5000, order=8, place=8, bounds=8, ws=256, bytes=1 << 30)
+    assert not bad(lib.fg_index_sort, sort, ["index", "order", "place", "bounds"])
+    look = dict(table=256, type=BF16, n=5, c=8, ts=8, index=8, m=3, scale=1.0, out=512, os=8)
+    assert not bad(lib.fg_lookup, look, ["index"])
+    back = dict(grad=256, type=BF16, m=10000, c=8, gs=8, index=8, order=8, bounds=8, n=5, scale=1.0, acc=0, to=256, gt=BF16, ts=8, ws=256, bytes=1 << 30)
+    assert not bad(lib.fg_lookup_backward, back, ["index", "order", "bounds"])
+    send = dict(x=256, type=BF16, t=5, c=8, xs=8, place=8, k=2, n=10, out=256, os=8)
+    assert not bad(lib.fg_dispatch, send, ["place"])
+    take = dict(rows=256, type=BF16, n=10, c=8, rs=8, index=8, w=8, t=5, k=2, walk=8, out=256, os=8)
+    assert not bad(lib.fg_combine, take, ["index", "w", "walk"])
+    grads = dict(grad=256, type=BF16, t=500, c=8, gs=8, rows=256, n=10, rs=8, index=8, w=8, k=2, order=8, bounds=8, walk=8, gr=256, grs=8, gw=8, ws=256, bytes=1 << 30)
+    assert not bad(lib.fg_combine_backward, grads, ["index", "w", "order", "bounds", "walk", "gw"])
