@@ -611,7 +611,7 @@ def _walk(t, n: int, device):
 def fg_combine(rows: torch.Tensor, index: torch.Tensor, weights: torch.Tensor | None = None, out: torch.Tensor | None = None,
                walk: torch.Tensor | None = None) -> torch.Tensor:
     """out[i] = sum_j weights[i, j] * rows[index[i, j]]: [t, c] of the rows' dtype.  walk [t]: the order in which they are made, a permutation
-    (for a graph, Binning.perm: several times as fast where the points are in no order)."""
+    (for a graph, Binning.perm: a third to a half of the time where the points are in no order)."""
     dev = rows.device
     at, stride = _row_view(rows, "rows")
     names = _index(index, "index", dev, 2)
@@ -631,7 +631,8 @@ def fg_combine_backward(grad_out: torch.Tensor, rows: torch.Tensor, index: torch
                         sort: IndexSort | None = None, grad_rows: torch.Tensor | None = None, grad_weights: torch.Tensor | None = None,
                         workspace: torch.Tensor | None = None, walk: torch.Tensor | None = None):
     """(gradient of rows, gradient of weights or None where there are none).  sort: fg_index_sort(index, len(rows)), needed where entries
-    share rows (walk [len(rows)]: the order in which they are taken, as for fg_combine); without it every row is named once at most, and rows that none names keep what grad_rows has (zeros if it is not given)."""
+    share rows (walk [len(rows)]: the order in which they are taken, as for fg_combine); without it every row is named once at most, and rows that none names keep what grad_rows has
+    (a new one, where it is not given, is filled with zeros first)."""
     dev = rows.device
     n, c = rows.shape
     at, stride = _row_view(rows, "rows")

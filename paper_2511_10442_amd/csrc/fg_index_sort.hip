@@ -17,8 +17,10 @@ namespace {
 
 constexpr int kMaxBits = 10;                 // of a digit: a million rows in two passes
 constexpr int kSmallBlock = 1024;
-// Entries that one workgroup sorts in LDS, where a row has two digits or more (8192 of 60000 rows 22 us in one launch, 20 in the four for more; with one
-// digit, 8192 of 256 rows, 14.6 and 7.9 in two).
+// Entries that one workgroup sorts in LDS, where a row has two digits or more.  us a call in this one launch / in the four for more, of 2000, 60000 and 1M
+// rows: 4097 entries 14.6 / 16.9, 16.4 / 18.5, 22 / 31; 6000 16.7 / 17.2, 18.6 / 18.7, 24 / 35; 8192 19.6 / 17.6, 21.9 / 18.9, 28 / 35.  Up to 60000 rows they meet
+// at some 6000 entries; from there to 8192 the one launch, which needs no workspace, loses 2 to 3 us and gains 7 and more where rows are many.  (With one digit
+// two launches are always less: 8192 of 256 rows 14.6 / 7.9.)
 constexpr int64_t kSmallM = 8192;
 // Entries that are counted, by 4 and by 16 lanes a question, and how many questions (entries and bounds) and looks at a key at most.  us counted by 4 /
 // counted by 16 / sorted in LDS: 64 entries of 8 rows 1.7 / 2.1 / 3.0, 300 of 50000 4.2 / 5.3 / 7.0, 100 of 200000 5.5 / 8.6 / 7.9, 1000 of 5003 7.2 / 4.0 / 7.2, 1024 of 20000

@@ -9,7 +9,9 @@ namespace {
 // ---- sums over the entries of a row ------------------------------------------------------------------------------------
 
 // Rows that are named often are summed in parts: `chunk` entries of the sorted index that all name one row, and kChunks such chunks, are summed
-// by themselves and put together afterwards, so that what one lane does for a row hardly grows with the row's entries.  chunk is kChunk.  Rows of a
+// by themselves and put together afterwards, so that one lane adds up some hundreds of a row's entries or parts.  (Beyond 500000 entries of one row it is thousands: the
+// join's lane has the chunks of chunks, 4096 at most, one after the other.  500000 entries of one row, 64 float32, 63 us, of which the join 34; 4M 458 and 251, where 4M
+// entries of 100000 rows take 209.)  chunk is kChunk.  Rows of a
 // graph are all named often, and as chunks they would be read by a few scattered lanes: there it grows to four times the mean of a row's
 // entries, as far as the rows alone give 512 lanes for every entry of a chunk, so that one lane's share stays small beside the whole (a power of two;
 // 20k points, 40 neighbours of 64 float32: 57 us with chunks of 32, 42 with 256; 9k points, 100 neighbours of 128 78 and 50; but entries whose rows follow
@@ -23,8 +25,8 @@ namespace {
 // Bound by memory: the gradient of 131072 x 2048 float32 from 64k tokens in bf16, the commonest of which comes 4000 times, takes 245 us + 13 for the
 // long rows (1.33 GB at 5.2 TB/s); 131072 x 4096 bf16 from 20k tokens 157, what filling it with zeros takes.  In a graph of 100k points with
 // 40 neighbours each, 64 float32 a point, 235 us with the weights' gradient: 125 for the points' rows (1 GB out of the last-level cache), 60 for a
-// weight and 50 for its gradient an entry, 4 bytes each in a line of its own.  (The products in a kernel of their own: 170 + 150.)  Taken in the order of
-// the points' bins (walk), 104.
+// weight and 50 for its gradient an entry, 4 bytes each in a line of its own.  (The products in a kernel of their own: 170 + 150.)  The 40 nearest
+// of 100k uniform points: 256, taken in the order of the points' bins (walk) 94.
 constexpr int kChunk = 32, kChunks = 32;
 constexpr int64_t kPartsFrom = 16;           // chunks of chunks from which on it is looked whether there are any
 
@@ -222,7 +224,8 @@ __global__ __launch_bounds__(kBlock, DOTS && sizeof(T) == 2 ? 3 : 4) void k_row_
 // Few entries, spread over many rows: a wavefront for 64 pieces of a row; where a row has more than kAlone entries after all, the workgroup's wavefronts
 // take a share of them each and meet in LDS.  Against chunks and their join, us (entries, rows x width): 1000 of 5003 x 257 float32 5.5 / 10.3, 500 of
 // 100 x 64 4.3 / 7.5, 100 of 30 x 512 3.3 / 4.6, 64 of 30000 x 256 10.5 / 11.3; but 1000 of 100 x 2048 17.9 / 15.3, 1000 of 3 x 300 21 / 10, 2000 of 2000 x
-// 4096 32 / 16.  (All 1000 of one row of many: 21 / 10.)
+// 4096 32 / 16.  (All 1000 of one row of many: 21 / 10.)  Lanes behind a row's last piece idle: 48 of 64 with 16 pieces, 63 of the second wavefront's with 65;
+// pieces one after the other over the lanes, as deal() would have them there, were not tried.
 constexpr int kFewBlock = 512, kAlone = 32;
 constexpr int64_t kFewEntries = 1024, kFewUnits = 32768;
 inline bool takes_few(int64_t m, int64_t n_rows, int64_t units) { return m <= kFewEntries && m <= 8 * n_rows && units <= kFewUnits; }

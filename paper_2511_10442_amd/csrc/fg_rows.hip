@@ -63,8 +63,8 @@ __global__ __launch_bounds__(kBlock) void k_dispatch(const T* __restrict__ x, in
 // out[i] = sum over j of weights[i][j] rows[index[i][j]], eight rows' pieces under way at a time.  Where every row is named once, 32k sums of 8 rows of
 // 4 KiB take 207 us (1.2 GB at 5.8 TB/s); messages along a graph, 200k points of 64 float32 with 40 neighbours each in no order, 282 us: 2 GB of
 // rows leave the last-level cache at 7.3 TB/s.  `walk` is the order in which the sums are made: points of a neighbourhood one after the other, on one XCD
-// (shared), find each other's neighbours in its L2.  200k points in three dimensions, 40 nearest neighbours: 294 us in no order, 103 in that of their
-// bins (100k: 137 and 52; 1M, 32 neighbours: 1234 and 541).
+// (shared), find each other's neighbours in its L2.  200k uniform points in three dimensions, 40 nearest neighbours: 291 us in no order, 97 in that of
+// their bins (100k: 137 and 53; 1M, 32 neighbours: 1234 and 530).
 // (n_rows > 0: an entry that names no row reads row 0 and adds zeros in its place, so that no load waits behind a branch)
 template <typename T, int N, bool WEIGHTED, bool STREAM, int SEGS>
 __global__ __launch_bounds__(kBlock) void k_combine(const T* __restrict__ rows, int64_t rows_stride, uint32_t n_rows, const int32_t* __restrict__ index,
